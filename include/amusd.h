@@ -53,6 +53,8 @@ extern "C" {
                                   * (same 2 bytes, three more mantissa bits): keys, values and queries are assumed to
                                   * lie within +-65504 and are clamped to that range when stored */
 
+#define AMUSD_DTYPE_INT8    2   /* signed 8 bits with fp32 scales (the 8-bit operators) */
+
 #define AMUSD_MAX_K        16   /* rows of one pass: the 16-row matrix-core tile */
 #define AMUSD_MAX_SEQS   4096   /* sequences (key-value caches) one model can hold */
 
@@ -269,6 +271,86 @@ int amusd_generate_sync(amusd_model *draft, amusd_model *verify, const int32_t *
  * prefill, then one single-row pass per token. */
 int amusd_generate_greedy(amusd_model *m, const int32_t *prompt, int32_t n_prompt, int32_t n_new,
                           int32_t *out_tokens, amusd_loop_stats *stats);
+
+/* ---- operators of 8-bit decoders, on device memory ------------------------------------------- */
+/* Not in the paper.  A pass is bound by the bytes of its weights and, far into a context, of its cache; these are
+ * the parts of a decoder layer that holds both in 8 bits: rows to 8 bits, with or without an RMS norm in front, the
+ * product of such rows with an 8-bit matrix, and attention over a cache in 8 bits.
+ *
+ * 8 bits stand for x ~ q * s, q an integer in [-127, 127]: s = max|x| / 127 over the values that share the scale, q = x / s
+ * rounded to the nearest integer, ties to even.  s = 0 where all values are 0.  Values that are not finite give
+ * s = NaN and q = 0, so that what is computed from them is NaN too.
+ *
+ * All pointers are device memory of the current device unless said otherwise, but arrays of sequence ids, positions and
+ * counts are host memory and may be reused when the call returns.  Calls enqueue their work on `hip_stream` and do not
+ * wait for it; they allocate nothing and may be captured into a graph (the host arrays' values are then part of it).
+ * Handles are made, filled and released outside of captures (these calls wait for their stream), and used with the
+ * device current on which they were made (else ARG).  ld* are distances between rows, in elements.  Calls that read a
+ * matrix may overlap; calls on one cache must not, on whatever streams. */
+
+/* Rows to 8 bits: q[r][0..n) and scale[r] from x[r][0..n), x fp32 or bf16 (dtype) of any alignment of its type.
+ * q has to be 16-byte aligned and ldq a multiple of 16; bytes past n of a row are left as they are.  rows may be 0. */
+int amusd_q8_quantize(const void *x, int32_t dtype, int64_t ldx, int32_t rows, int32_t n, int8_t *q, int64_t ldq,
+                      float *scale, void *hip_stream);
+
+/* The RMS norm in front of a projection: s = x + add (add may be NULL; fp32 or bf16, add_dtype), sum = s in x's type (sum may
+ * be NULL, or x itself), y = s / sqrt(mean(s^2) + eps) * gain, and y in 8 bits as amusd_q8_quantize has it.  Squares and
+ * norms are taken in 64 bits, from s before it is rounded to sum.  gain: fp32 [n].  sum = x in bf16: n at most 16384. */
+int amusd_q8_rmsnorm(const void *x, int32_t dtype, int64_t ldx, const void *add, int32_t add_dtype, int64_t ldadd,
+                     const float *gain, float eps, int32_t rows, int32_t n, void *sum, int64_t ldsum, int8_t *q,
+                     int64_t ldq, float *scale, void *hip_stream);
+
+/* A matrix of n output features and k columns in 8 bits with a scale for each feature, in the order that the product reads it.
+ * w: row-major [n][ld], fp32 or bf16 (rounded to 8 bits here; scale is NULL), or 8-bit integers in [-127, 127] with
+ * their scales; host (on_device = 0) or device memory, not referenced after the call.  gated: the first n/2 features are the
+ * gate's and the others the up projection's of a SwiGLU, and the product gives silu(gate) * up, n/2 columns.
+ * k is at most 131072 (sums stay inside 32 bits). */
+typedef struct amusd_q8_matrix amusd_q8_matrix;
+int amusd_q8_matrix_create(const void *w, int32_t dtype, const float *scale, int32_t n, int32_t k, int64_t ld,
+                           int32_t gated, int32_t on_device, void *hip_stream, amusd_q8_matrix **out);
+int amusd_q8_matrix_free(amusd_q8_matrix *m);
+
+/* out[r][c] = scale[r] * (the matrix's scale of c) * sum over i of x[r][i] * w[c][i], the sum exact; out fp32 or bf16.
+ * x: 8-bit rows as the calls above leave them (16-byte aligned, ldx a multiple of 16; a row's ldx bytes are
+ * readable, those past k are not used).  A row's bits do not depend on the number of rows.  rows may be 0.
+ * workspace: device memory of amusd_q8_gemm_workspace_bytes(w, rows), 16-byte aligned, zeros before its first use and
+ * again after each call; calls that overlap need one each.  Without one (NULL, or too small) a product of few rows and few
+ * features takes longer, with the same bits. */
+int64_t amusd_q8_gemm_workspace_bytes(const amusd_q8_matrix *w, int32_t rows);
+int amusd_q8_gemm(const amusd_q8_matrix *w, const int8_t *x, int64_t ldx, const float *scale, int32_t rows, void *out,
+                  int32_t dtype, int64_t ldo, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/* The key-value caches of n_layers layers and n_seqs sequences in 8 bits, capacity positions each, with a scale for every `block`
+ * positions (1, 16, 32 or 64) of a kv head's keys, and one of its values.  Also holds the memory that attention of few rows
+ * needs.  Head counts and head_dim as in amusd_config.  Zeroed. */
+typedef struct amusd_q8_cache amusd_q8_cache;
+int amusd_q8_cache_create(int32_t n_layers, int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                          int32_t capacity, int32_t block, void *hip_stream, amusd_q8_cache **out);
+int amusd_q8_cache_free(amusd_q8_cache *c);
+
+/* Appends to n_seq (1 to 16) distinct sequences: n[i] rows of sequence seq_ids[i] at its positions pos0[i] .., what it held there and
+ * behind is forgotten.  k, v: bf16 rows [n_kv_heads * head_dim], the sequences' back to back.  rope_cos, rope_sin: fp32
+ * tables [position][head_dim / 2] by which keys are turned (pairs i, i + head_dim/2) before they are rounded, or
+ * both NULL.  A block that holds positions in front of pos0 keeps its scale unless a new value needs a larger one; what
+ * it holds is then rounded again, to the larger scale.  With block = 1 nothing that is held ever changes.
+ * Errors: ARG, RANGE (pos0 < 0), CAPACITY. */
+int amusd_q8_cache_append(amusd_q8_cache *c, int32_t layer, int32_t n_seq, const int32_t *seq_ids, const int32_t *pos0,
+                          const int32_t *n, const void *k, const void *v, int64_t ld, const float *rope_cos,
+                          const float *rope_sin, void *hip_stream);
+
+/* The values that positions pos0[i] .. pos0[i] + n[i] - 1 stand for, in rows as append takes them, fp32 or bf16. */
+int amusd_q8_cache_read(const amusd_q8_cache *c, int32_t layer, int32_t n_seq, const int32_t *seq_ids,
+                        const int32_t *pos0, const int32_t *n, void *k, void *v, int32_t dtype, int64_t ld,
+                        void *hip_stream);
+
+/* Causal attention: row j of sequence seq_ids[i] stands at position pos0[i] + j and sees that sequence's positions up to its own,
+ * which have to be in the cache (its own too).  out = softmax(scale * q . k) v, q and out bf16 rows
+ * [n_q_heads * head_dim], q turned by the tables as keys are.  A query is rounded to 16 bits of its largest
+ * component, softmax weights to 11 bits; sums are fp32.  A row's bits depend on its query and on what it sees, not on the
+ * call's other rows. */
+int amusd_q8_attention(amusd_q8_cache *c, int32_t layer, int32_t n_seq, const int32_t *seq_ids, const int32_t *pos0,
+                       const int32_t *n, const void *q, int64_t ldq, float scale, const float *rope_cos,
+                       const float *rope_sin, void *out, int64_t ldo, void *hip_stream);
 
 /* ---- inspection (tests, benchmark) ---------------------------------------------------------- */
 

@@ -13,7 +13,7 @@ os.environ.setdefault("HIP_FORCE_DEV_KERNARG", "1")
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.environ.get("AMUSD_LIBRARY") or os.path.join(_HERE, "libamusd.so")
 
-DTYPE_FP32, DTYPE_BF16 = 0, 1
+DTYPE_FP32, DTYPE_BF16, DTYPE_INT8 = 0, 1, 2
 MAX_K = 16
 OPT_KEEP_LOGITS, OPT_TIME_STAGE, OPT_PREFILL_WORKSPACE = 0, 2, 3
 STAGES = {"embed": 0, "qkv": 1, "attention": 2, "attn_merge": 3, "oproj": 4, "gateup": 5, "down": 6,
@@ -64,7 +64,7 @@ def _load():
         raise ImportError(f"{_LIB_PATH} is missing: build it with `python paper_2410_17375_amd/build.py` "
                           "(there is no CPU fallback)")
     L = C.CDLL(_LIB_PATH)
-    vp, i32, i32p, f32p = C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_float)
+    vp, i32, i64, i32p, f32p = C.c_void_p, C.c_int32, C.c_int64, C.POINTER(C.c_int32), C.POINTER(C.c_float)
     sig = {
         "amusd_model_create": (C.c_int, [C.POINTER(Config), vp, C.POINTER(vp)]),
         "amusd_model_set_tensor": (C.c_int, [vp, i32, i32, vp, i32]),
@@ -102,6 +102,17 @@ def _load():
         "amusd_kv_bytes_per_pass": (C.c_int64, [vp, i32, i32]),
         "amusd_calibration_copy": (C.c_int, [vp, vp, C.c_int64, vp]),
         "amusd_calibration_chain": (C.c_int, [vp, C.c_int64, C.c_int64, i32, vp, vp]),
+        "amusd_q8_quantize": (C.c_int, [vp, i32, i64, i32, i32, vp, i64, vp, vp]),
+        "amusd_q8_rmsnorm": (C.c_int, [vp, i32, i64, vp, i32, i64, vp, C.c_float, i32, i32, vp, i64, vp, i64, vp, vp]),
+        "amusd_q8_matrix_create": (C.c_int, [vp, i32, vp, i32, i32, i64, i32, i32, vp, C.POINTER(vp)]),
+        "amusd_q8_matrix_free": (C.c_int, [vp]),
+        "amusd_q8_gemm_workspace_bytes": (i64, [vp, i32]),
+        "amusd_q8_gemm": (C.c_int, [vp, vp, i64, vp, i32, vp, i32, i64, vp, i64, vp]),
+        "amusd_q8_cache_create": (C.c_int, [i32, i32, i32, i32, i32, i32, i32, vp, C.POINTER(vp)]),
+        "amusd_q8_cache_free": (C.c_int, [vp]),
+        "amusd_q8_cache_append": (C.c_int, [vp, i32, i32, i32p, i32p, i32p, vp, vp, i64, vp, vp, vp]),
+        "amusd_q8_cache_read": (C.c_int, [vp, i32, i32, i32p, i32p, i32p, vp, vp, i32, i64, vp]),
+        "amusd_q8_attention": (C.c_int, [vp, i32, i32, i32p, i32p, i32p, vp, i64, C.c_float, vp, vp, vp, i64, vp]),
         "amusd_strerror": (C.c_char_p, [C.c_int]),
         "amusd_last_error": (C.c_char_p, []),
     }
@@ -289,6 +300,86 @@ def calibration_copy(dst_ptr, src_ptr, nbytes, stream=0):
 def calibration_chain(buf_ptr, buf_bytes, bytes_per_kernel, n_kernels, scratch_ptr, stream=0):
     _check(lib.amusd_calibration_chain(C.c_void_p(buf_ptr), buf_bytes, bytes_per_kernel, n_kernels,
                                        C.c_void_p(scratch_ptr), C.c_void_p(stream)))
+
+
+# ---- operators of 8-bit decoders.  Addresses are integers: device memory, 0 for NULL.
+
+def q8_quantize(x, dtype, ldx, rows, n, q, ldq, scale, stream=0):
+    _check(lib.amusd_q8_quantize(x, dtype, ldx, rows, n, q, ldq, scale, stream))
+
+
+def q8_rmsnorm(x, dtype, ldx, add, add_dtype, ldadd, gain, eps, rows, n, sum, ldsum, q, ldq, scale, stream=0):
+    _check(lib.amusd_q8_rmsnorm(x, dtype, ldx, add, add_dtype, ldadd, gain, eps, rows, n, sum, ldsum, q, ldq, scale, stream))
+
+
+class Q8Matrix:
+    """Handle of one amusd_q8_matrix.  w (and scale, with 8-bit weights): numpy arrays (host) or device addresses."""
+
+    def __init__(self, w, dtype, n, k, scale=None, ld=None, gated=False, on_device=False, stream=0):
+        if not on_device:
+            w = np.ascontiguousarray(w)
+            keep = None if scale is None else np.ascontiguousarray(scale, dtype=np.float32)
+            ptr, scale = w.ctypes.data, 0 if keep is None else keep.ctypes.data
+        else:
+            ptr = int(w)
+        self._h = C.c_void_p()
+        _check(lib.amusd_q8_matrix_create(ptr, dtype, scale, n, k, k if ld is None else ld, 1 if gated else 0,
+                                          1 if on_device else 0, stream, C.byref(self._h)))
+
+    def workspace_bytes(self, rows):
+        return int(lib.amusd_q8_gemm_workspace_bytes(self._h, rows))
+
+    def free(self):
+        if self._h:
+            lib.amusd_q8_matrix_free(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def q8_gemm(matrix, x, ldx, scale, rows, out, dtype, ldo, workspace=0, workspace_bytes=0, stream=0):
+    _check(lib.amusd_q8_gemm(matrix._h, x, ldx, scale, rows, out, dtype, ldo, workspace, workspace_bytes, stream))
+
+
+class Q8Cache:
+    """Handle of one amusd_q8_cache.  seq_ids, pos0, n: one entry per sequence of the call."""
+
+    def __init__(self, *, n_layers, n_seqs, n_q_heads, n_kv_heads, head_dim, capacity, block=1, stream=0):
+        self._h = C.c_void_p()
+        _check(lib.amusd_q8_cache_create(n_layers, n_seqs, n_q_heads, n_kv_heads, head_dim, capacity, block, stream,
+                                         C.byref(self._h)))
+
+    @staticmethod
+    def _seqs(seq_ids, pos0, n):
+        if not len(seq_ids) == len(pos0) == len(n):
+            raise ValueError("seq_ids, pos0 and n differ in length")
+        a = C.c_int32 * len(seq_ids)
+        return len(seq_ids), a(*seq_ids), a(*pos0), a(*n)
+
+    def append(self, layer, seq_ids, pos0, n, k, v, ld, rope_cos=0, rope_sin=0, stream=0):
+        _check(lib.amusd_q8_cache_append(self._h, layer, *self._seqs(seq_ids, pos0, n), k, v, ld, rope_cos, rope_sin, stream))
+
+    def read(self, layer, seq_ids, pos0, n, k, v, dtype, ld, stream=0):
+        _check(lib.amusd_q8_cache_read(self._h, layer, *self._seqs(seq_ids, pos0, n), k, v, dtype, ld, stream))
+
+    def attention(self, layer, seq_ids, pos0, n, q, ldq, scale, rope_cos, rope_sin, out, ldo, stream=0):
+        _check(lib.amusd_q8_attention(self._h, layer, *self._seqs(seq_ids, pos0, n), q, ldq, scale, rope_cos, rope_sin, out,
+                                      ldo, stream))
+
+    def free(self):
+        if self._h:
+            lib.amusd_q8_cache_free(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
 
 
 def _loop(fn, models, prompt, n_new, k_max):

@@ -18,6 +18,7 @@
 
 #include "amusd_launch.h"
 #include "amusd_loops.h"
+#include "amusd_q8.h"
 
 using namespace amusd;
 
@@ -36,6 +37,22 @@ int fail(int code, const std::string& msg) {
         if (e_ != hipSuccess)                                                                           \
             return fail(AMUSD_E_HIP, std::string(#expr) + ": " + hipGetErrorString(e_));                \
     } while (0)
+
+}  // namespace
+
+namespace amusd {
+int report(int code, const char* what, const char* detail) {
+    try {
+        g_last_error = what;
+        if (detail) g_last_error.append(": ").append(detail);
+    } catch (const std::bad_alloc&) {
+        g_last_error.clear();
+    }
+    return code;
+}
+}  // namespace amusd
+
+namespace {
 
 struct HostStage {          // pinned: what one pass receives from the device
     PassResult res;

@@ -1,0 +1,72 @@
+// The operators of 8-bit models: rows to 8 bits (with or without an RMS norm), products of 8-bit integers, a key-value cache in
+// 8 bits and its attention.  Types shared by their kernels and host code, and the host-callable launchers.
+//
+// 8 bits here: symmetric signed integers and an fp32 scale, x ~ q * s with s = max|x| / 127 over what shares the scale and
+// q = x / s rounded to nearest even.  s = 0 stands for zeros; values that are not finite make s NaN (and q 0), so that whatever
+// reads them is NaN as well.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/amusd.h"
+#include "amusd_dev.h"
+
+// Opaque handles of the C interface.
+struct amusd_q8_matrix {
+    const uint4* frag = nullptr;   // [tile of 16 features][K / 64][64 lanes] x 16 B: lane l holds feature l%16, K bytes (l/16)*16 ..
+                                   // of the block; features past n and columns past k are zeros.  Gated: tile 2t gate, 2t+1 up
+    const float* scale = nullptr;  // [tiles * 16], same order
+    int n = 0, k = 0;              // output columns (gated: half the features), contraction
+    int tiles = 0, kblocks = 0, gated = 0, device = 0, cus = 0;
+};
+
+struct amusd_q8_cache {
+    int n_layers = 0, n_seqs = 0, Hq = 0, Hkv = 0, hd = 0, G = 0, cap = 0, block = 1, device = 0, cus = 0;
+    int chunk = 0;                 // keys of a chunk: its sums are complete before they are merged
+    int max_chunks = 0, part_tiles = 0;
+    int8_t* k = nullptr;           // [layer][seq][kv head][cap][hd]
+    int8_t* v = nullptr;           // [layer][seq][kv head][cap/32][hd/32][64 lanes][16]: operand order (q8_v_index)
+    float* ks = nullptr;           // [layer][seq][kv head][cap/block]
+    float* vs = nullptr;
+    float* part = nullptr;         // [part_tiles][max_chunks][hd + 2][16]: numerators, reference, denominator of 16 pairs
+};
+
+namespace amusd {
+
+// Keeps a message for amusd_last_error and returns the code.
+int report(int code, const char* what, const char* detail = nullptr);
+
+constexpr int kQ8MaxK = 1 << 17;     // columns of a contraction: its sum of products of 127 * 127 stays inside 32 bits
+constexpr int kQ8MaxRow = 2 * 8 * 1024;   // columns of a row that a workgroup keeps in registers
+constexpr int kQ8Group = 64;       // positions an append workgroup owns; the cache's capacity is a multiple of it
+
+// A sequence's share of a call: rows row0 .. row0+n-1 are its positions pos0 .. pos0+n-1.
+struct Q8Seg {
+    int seq, pos0, n, row0;
+    int unit0;                     // its first unit of work (append: groups of 64 positions; attention: tiles of pairs)
+};
+struct Q8Segs {
+    int n_seg, rows, units, max_len;
+    Q8Seg s[kMaxSegs];
+};
+
+// Byte of (position, column) in a kv head's values.  The 8 keys of a lane are those whose scores the lane holds: the weights then
+// are the matrix instruction's operand as they come.
+__host__ __device__ inline size_t q8_v_index(int hd, int pos, int c) {
+    return (((size_t)(pos >> 5) * (hd >> 5) + (c >> 5)) * 64 + ((pos & 15) >> 2) * 16 + (c & 15)) * 16 + ((c >> 4) & 1) * 8 + ((pos >> 4) & 1) * 4 +
+           (pos & 3);
+}
+
+hipError_t launch_q8_rows(const void* x, int dtype, int64_t ldx, const void* add, int add_dtype, int64_t ldadd, const float* gain, float eps, int rows,
+                          int n, void* sum, int64_t ldsum, int8_t* q, int64_t ldq, float* scale, hipStream_t stream);
+hipError_t launch_q8_gemm(const amusd_q8_matrix& w, const int8_t* x, int64_t ldx, const float* scale, int rows, void* out, int dtype, int64_t ldo,
+                          void* work, int64_t work_bytes, hipStream_t stream);
+int64_t q8_gemm_workspace(const amusd_q8_matrix& w, int rows);
+void q8_attention_plan(amusd_q8_cache& c);        // chunk, max_chunks and part_tiles from the sizes
+hipError_t launch_q8_append(const amusd_q8_cache& c, int layer, const Q8Segs& S, const void* k, const void* v, int64_t ld, const float* cos,
+                            const float* sin, hipStream_t stream);
+hipError_t launch_q8_read(const amusd_q8_cache& c, int layer, const Q8Segs& S, void* k, void* v, int dtype, int64_t ld, hipStream_t stream);
+hipError_t launch_q8_attention(const amusd_q8_cache& c, int layer, const Q8Segs& S, const void* q, int64_t ldq, float scale, const float* cos,
+                               const float* sin, void* out, int64_t ldo, hipStream_t stream);
+
+}  // namespace amusd

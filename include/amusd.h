@@ -53,14 +53,16 @@ extern "C" {
                                   * (same 2 bytes, three more mantissa bits): keys, values and queries are assumed to
                                   * lie within +-65504 and are clamped to that range when stored */
 
-#define AMUSD_DTYPE_INT8    2   /* signed 8 bits with fp32 scales (the 8-bit operators) */
-
+#define AMUSD_DTYPE_INT8    2   /* an 8-bit model: tensors come in bf16 as with AMUSD_DTYPE_BF16, matrices and cache are held as signed 8 bits with
+                                  * fp32 scales (a feature, a position and kv head), embedding and gains as they are.  A pass is the 8-bit operators
+                                  * below one after the other.  It is another model than the bf16 one of the same tensors, and keeps
+                                  * the same promises: exact loops, rows whose bits depend on their sequence alone */
 #define AMUSD_MAX_K        16   /* rows of one pass: the 16-row matrix-core tile */
 #define AMUSD_MAX_SEQS   4096   /* sequences (key-value caches) one model can hold */
 
 /* Tensor ids for amusd_model_set_tensor.  Matrices are row-major
  * [out_features, in_features] in the model's dtype (bf16 bit patterns or
- * fp32); gains are [d_model] in the same dtype. */
+ * fp32; bf16 for an 8-bit model); gains are [d_model] in the same dtype. */
 enum {
     AMUSD_T_EMBED = 0,      /* [vocab, d_model]                  (no layer) */
     AMUSD_T_LM_HEAD = 1,    /* [vocab, d_model]                  (no layer) */
@@ -81,7 +83,8 @@ enum {
 enum {
     AMUSD_OPT_KEEP_LOGITS = 0, /* 1: each pass also stores its fp32 logits (test hook), default 0.  The first time it takes a
                                   pinned host block of at most 4 MB, which the model keeps */
-    AMUSD_OPT_TIME_STAGE = 2,   /* AMUSD_STAGE_* to bracket with HIP events in every pass, -1: none (default) */
+    AMUSD_OPT_TIME_STAGE = 2,   /* AMUSD_STAGE_* to bracket with HIP events in every pass, -1: none (default).  8-bit models: ATTENTION holds the
+                                  merge, and rounding to 8 bits, norms and appending belong to no stage */
     AMUSD_OPT_PREFILL_WORKSPACE = 3 /* 0: the prefill workspace (amusd_prefill) is given back, or not taken by finalize;
                                        1: taken (default; HIP error if there is no memory for it) */
 };
@@ -96,7 +99,7 @@ enum {
 typedef struct amusd_model amusd_model; /* opaque, owned by the library */
 
 /* Decoder shape.  Requirements: n_q_heads / n_kv_heads is 1, 2, 4 or 8; head_dim is 64 or
- * 128; d_model, n_q_heads*head_dim and d_ffn are multiples of 32 (bf16) or 16
+ * 128; d_model, n_q_heads*head_dim and d_ffn are multiples of 32 (bf16, int8) or 16
  * (fp32); vocab and d_ffn multiples of 16; 1 <= max_k <= AMUSD_MAX_K;
  * 0 <= max_seqs <= AMUSD_MAX_SEQS. */
 typedef struct {
@@ -158,7 +161,7 @@ int amusd_model_free(amusd_model *m);
  * be NULL.  Errors: ARG, TOKEN, CAPACITY.
  * A prompt of more tokens than a verify pass is given (max_k, with 16-bit weights at most 8) goes through up to
  * 2048 rows at a time, in a workspace that amusd_model_finalize takes: about 0.5 GB for a 1B shape, 0.7 GB for an
- * 8B shape, less for a max_ctx below 2048.  A model that finds no memory for it, or is told to hold none
+ * 8B shape, less for a max_ctx below 2048 (8-bit models: about 0.3 GB for an 8B shape).  A model that finds no memory for it, or is told to hold none
  * (AMUSD_OPT_PREFILL_WORKSPACE), takes its prompts in verify passes instead: the same bits, 4 to 14 times the time.
  * So does a prompt while AMUSD_OPT_TIME_STAGE selects a stage.  When a model's weights or cache find no memory, the
  * library gives back idle models' workspaces on that GPU; the option takes them again. */
@@ -190,7 +193,8 @@ int amusd_verify(amusd_model *m, int32_t ctx_len, const int32_t *draft, int32_t 
  * very wide models) is refused with AMUSD_E_CAPACITY and unchanged state.  All models on one GPU share the
  * array and it keeps the last call's contents (the region is cleared when another model used it last), so two
  * amusd_verify_static calls that overlap in time on one GPU race, also when they are for different models on
- * different streams.  Inputs (weights, cache, drafts) and outputs are where amusd_verify has them. */
+ * different streams.  Inputs (weights, cache, drafts) and outputs are where amusd_verify has them.  (8-bit models keep
+ * the partial sums of attention with their cache.) */
 #define AMUSD_STATIC_SCRATCH_BYTES (16 * 1024 * 1024)
 int amusd_verify_static(amusd_model *m, int32_t ctx_len, const int32_t *draft, int32_t k,
                         int32_t *accept_len, int32_t *next_token);

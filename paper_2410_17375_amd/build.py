@@ -7,7 +7,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libamusd.so")
 SOURCES = ["amusd_kernels.hip", "amusd_prefill.hip", "amusd_q8.hip", "amusd_q8_gemm.hip", "amusd_q8_attention.hip",
-           "amusd_host.hip"]
+           "amusd_q8_model.hip", "amusd_host.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Wno-pass-failed",

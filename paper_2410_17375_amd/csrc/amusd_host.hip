@@ -129,6 +129,8 @@ struct amusd_model {
     std::mutex export_mutex;
     PrefillBufs pf{};                      // workspace of the prefill pass; cap 0: prompts go through the verify pass
     PfTileSet pf_tiles[kPfStages];
+    Q8Model* q8 = nullptr;                 // AMUSD_DTYPE_INT8: matrices and cache
+    Q8Bufs q8_bufs{}, q8_static{}, q8_pf{};   // buffers of a verify pass, of one in the static array, of a prefill pass
     void* pf_mem = nullptr;                // the device allocation that its buffers are in
     size_t pf_bytes = 0;
     bool want_prefill = true;              // AMUSD_OPT_PREFILL_WORKSPACE
@@ -143,9 +145,12 @@ struct amusd_model {
     double stage_ms = 0.0;
     int64_t stage_launches = 0;
     int64_t last_positions = 0;             // cache positions the last pass's attention read, all sequences
-    int esz() const { return cfg.dtype == AMUSD_DTYPE_BF16 ? 2 : 4; }
-    int kb() const { return cfg.dtype == AMUSD_DTYPE_BF16 ? 32 : 16; }
-    int block_keys() const { return cfg.dtype == AMUSD_DTYPE_BF16 ? 32 : 16; }
+    int esz() const { return cfg.dtype == AMUSD_DTYPE_FP32 ? 4 : 2; }      // of tensors as they come (8-bit models: bf16)
+    int kb() const { return cfg.dtype == AMUSD_DTYPE_FP32 ? 16 : 32; }
+    int block_keys() const { return cfg.dtype == AMUSD_DTYPE_FP32 ? 16 : 32; }
+    // bytes of a matrix as a pass reads it (8 bits: with its scales), and of a position of one kv head's keys or values
+    int64_t matrix_bytes(int64_t features, int64_t k) const { return features * k * (q8 ? 1 : esz()) + (q8 ? features * 4 : 0); }
+    int64_t position_bytes() const { return q8 ? cfg.head_dim + 4 : (int64_t)cfg.head_dim * esz(); }
 };
 
 namespace {
@@ -192,7 +197,7 @@ int check_config(const amusd_config* c) {
     if (c->n_layers < 1 || c->d_model < 1 || c->n_q_heads < 1 || c->n_kv_heads < 1 || c->d_ffn < 1 || c->vocab < 1 ||
         c->max_ctx < 1)
         return fail(AMUSD_E_ARG, "config: non-positive dimension");
-    if (c->dtype != AMUSD_DTYPE_FP32 && c->dtype != AMUSD_DTYPE_BF16) return fail(AMUSD_E_ARG, "config: unknown dtype");
+    if (c->dtype != AMUSD_DTYPE_FP32 && c->dtype != AMUSD_DTYPE_BF16 && c->dtype != AMUSD_DTYPE_INT8) return fail(AMUSD_E_ARG, "config: unknown dtype");
     if (c->max_k < 1 || c->max_k > AMUSD_MAX_K) return fail(AMUSD_E_ARG, "config: max_k outside [1,16]");
     if (c->max_seqs < 0 || c->max_seqs > AMUSD_MAX_SEQS) return fail(AMUSD_E_ARG, "config: max_seqs outside [0, AMUSD_MAX_SEQS]");
     if (c->head_dim != 64 && c->head_dim != 128) return fail(AMUSD_E_ARG, "config: head_dim must be 64 or 128");
@@ -202,7 +207,7 @@ int check_config(const amusd_config* c) {
         if (G != 1 && G != 2 && G != 4 && G != 8)
             return fail(AMUSD_E_ARG, "config: n_q_heads / n_kv_heads must be 1, 2, 4 or 8");
     }
-    const int kb = c->dtype == AMUSD_DTYPE_BF16 ? 32 : 16;
+    const int kb = c->dtype == AMUSD_DTYPE_FP32 ? 16 : 32;
     const long qdim = (long)c->n_q_heads * c->head_dim;
     if (c->d_model % kb || qdim % kb || c->d_ffn % kb)
         return fail(AMUSD_E_ARG, "config: d_model, n_q_heads*head_dim and d_ffn must be multiples of the fragment width");
@@ -334,7 +339,9 @@ int run_pass(amusd_model* m, const SegReq* segs, int n_seg, bool force_accept, b
     P.export_bytes = last ? export_with_pass(m, rows) : 0;
     m->exported = 0;
     HIP_TRY(hipEventRecord(m->ev0, m->stream));
-    HIP_TRY(launch_pass(D, m->layers_host.data(), P, m->nwg, m->stream, m->timer.stage >= 0 ? &m->timer : nullptr));
+    StageTimer* const timer = m->timer.stage >= 0 ? &m->timer : nullptr;
+    if (m->q8) HIP_TRY(q8_model_pass(m->q8, D, m->layers_host.data(), use_static ? m->q8_static : m->q8_bufs, P, m->stream, timer));
+    else HIP_TRY(launch_pass(D, m->layers_host.data(), P, m->nwg, m->stream, timer));
     HIP_TRY(hipEventRecord(m->ev1, m->stream));
     HIP_TRY(hipStreamSynchronize(m->stream));
     HIP_TRY(hipEventElapsedTime(&m->last_ms, m->ev0, m->ev1));
@@ -451,7 +458,7 @@ int take_prefill(amusd_model* m) {
     if (T.att_tiles > T.cap / 16) T.att_tiles = T.cap / 16;
     std::vector<int> orders;                       // the stages' tile orders back to back
     try {
-        for (int s = 0; s < kPfStages; ++s) prefill_tile_orders(D, s, m->nwg, orders, m->pf_tiles[s]);
+        for (int s = 0; s < kPfStages && !m->q8; ++s) prefill_tile_orders(D, s, m->nwg, orders, m->pf_tiles[s]);
         g_pf_holders.reserve(g_pf_holders.size() + 1);
     } catch (const std::bad_alloc&) {
         return fail(AMUSD_E_NOMEM, "tile orders of the prefill pass");
@@ -463,6 +470,7 @@ int take_prefill(amusd_model* m) {
     T.xch_bytes = std::max(T.xch_bytes, std::min(kPfShareBytes, 16 * cap * widest * 4));
     int* dev_orders = nullptr;
     auto layout = [&](uintptr_t base) {            // sets the pointers, returns the bytes
+        if (m->q8) return q8_model_bufs(m->q8, D, T.cap, base, m->q8_pf);
         size_t off = 0;
         auto place = [&](size_t bytes) {
             void* p = reinterpret_cast<void*>(base + off);
@@ -492,7 +500,10 @@ int take_prefill(amusd_model* m) {
     if (e == hipSuccess) e = hipHostGetDevicePointer(&host_dev, m->pf_host, 0);
     if (e == hipSuccess) {
         layout(reinterpret_cast<uintptr_t>(m->pf_mem));
-        e = hipMemcpy(dev_orders, orders.data(), orders.size() * 4, hipMemcpyHostToDevice);
+        if (m->q8) {                               // (products leave their workspace as they find it: zeros)
+            e = m->q8_pf.work_bytes ? launch_fill_zero(static_cast<uint4*>(m->q8_pf.work), (size_t)m->q8_pf.work_bytes / 16, m->stream) : hipSuccess;
+            if (e == hipSuccess) e = hipStreamSynchronize(m->stream);
+        } else e = hipMemcpy(dev_orders, orders.data(), orders.size() * 4, hipMemcpyHostToDevice);
     }
     if (e != hipSuccess) {
         free_prefill(m);
@@ -518,7 +529,8 @@ int run_prefill(amusd_model* m, int seq, int L, const int32_t* tokens, int n, in
     m->exported = 0;
     std::memcpy(m->pf_host, tokens, (size_t)n * 4);
     HIP_TRY(hipEventRecord(m->ev0, m->stream));
-    HIP_TRY(launch_prefill(m->dm, m->layers_host.data(), m->pf, m->pf_tiles, P, m->stream));
+    if (m->q8) HIP_TRY(q8_model_prefill(m->q8, m->dm, m->layers_host.data(), m->q8_pf, m->pf, P, tail, m->stream));
+    else HIP_TRY(launch_prefill(m->dm, m->layers_host.data(), m->pf, m->pf_tiles, P, m->stream));
     HIP_TRY(hipEventRecord(m->ev1, m->stream));
     HIP_TRY(hipStreamSynchronize(m->stream));
     HIP_TRY(hipEventElapsedTime(&m->last_ms, m->ev0, m->ev1));
@@ -636,7 +648,8 @@ int amusd_model_create(const amusd_config* cfg, void* hip_stream, amusd_model** 
         D.split_down = !long_k || pairs > kSplitTickets ? 0 : 2 * tiles <= m->nwg ? 1 : tiles == m->nwg ? 2 : 0;
     }
     const int lm_tiles = c.vocab / 16;
-    D.lm_wgs = lm_tiles < m->nwg ? lm_tiles : m->nwg;
+    const bool q8 = c.dtype == AMUSD_DTYPE_INT8;
+    D.lm_wgs = q8 ? kQ8LmParts : lm_tiles < m->nwg ? lm_tiles : m->nwg;
 
     m->seqs.resize(m->n_seqs);
     for (SeqState& q : m->seqs) q.greedy_at.assign((size_t)c.max_ctx + kRows + 1, -1);
@@ -650,6 +663,11 @@ int amusd_model_create(const amusd_config* cfg, void* hip_stream, amusd_model** 
     dst = reinterpret_cast<type>(p);
     for (int l = 0; l < c.n_layers; ++l) {
         DevLayer& Ly = m->layers_host[l];
+        if (q8) {
+            ALLOC(Ly.g_attn, const float*, d * 4, false)
+            ALLOC(Ly.g_mlp, const float*, d * 4, false)
+            continue;
+        }
         ALLOC(Ly.wqkv, const uint4*, (size_t)D.nqkv * d * esz, false)
         ALLOC(Ly.wo, const uint4*, d * q * esz, false)
         ALLOC(Ly.wgu, const uint4*, 2 * F * d * esz, false)
@@ -661,26 +679,35 @@ int amusd_model_create(const amusd_config* cfg, void* hip_stream, amusd_model** 
     }
     ALLOC(D.layers, const DevLayer*, sizeof(DevLayer) * c.n_layers, false)
     ALLOC(D.embed, const void*, V * d * esz, false)
-    ALLOC(D.wlm, const uint4*, V * d * esz, false)
+    if (!q8) { ALLOC(D.wlm, const uint4*, V * d * esz, false) }
     ALLOC(D.g_final, const float*, d * 4, false)
     ALLOC(D.rope_cos, const float*, (size_t)D.ctx_pad * (D.hd / 2) * 4, false)
     ALLOC(D.rope_sin, const float*, (size_t)D.ctx_pad * (D.hd / 2) * 4, false)
-    ALLOC(D.X, float*, kRows * d * 4, true)
-    ALLOC(D.A, void*, kRows * d * 4, true)
-    ALLOC(D.ssq, float*, (d / 16) * kRows * 4, true)
-    ALLOC(D.Q_hi, void*, kRows * q * 4, true)
-    ALLOC(D.Q_lo, void*, kRows * q * 4, true)
     const size_t pass_seqs = D.n_slots < kMaxSegs ? D.n_slots : kMaxSegs;
     const size_t att_part_bytes = pass_seqs * D.Hkv * D.max_chunks * D.G * kRows * (D.hd + 4) * 4;
-    ALLOC(D.att_part, float*, att_part_bytes, true)
     const size_t xch_bytes = (size_t)D.d / 16 * kSplitWaysMax * 256 * 4;    // a partial tile per tile and K range
-    ALLOC(D.xch, float*, xch_bytes, true)
-    ALLOC(D.xch_ticket, int*, kSplitTickets * 4, true)
-    ALLOC(D.O, void*, kRows * q * 4, true)
-    ALLOC(D.H, void*, kRows * F * 4, true)
+    const size_t best_bytes = (size_t)std::max(m->nwg, D.lm_wgs) * kRows * 4;
+    if (q8) {
+        if ((rc = q8_model_create(D, m->device, dev_malloc, m->stream, &m->q8)) != AMUSD_OK) return bail(rc);
+        const size_t bytes = q8_model_bufs(m->q8, D, kRows, 0, m->q8_bufs);
+        void* bufs = nullptr;
+        ALLOC(bufs, void*, bytes, true)
+        q8_model_bufs(m->q8, D, kRows, reinterpret_cast<uintptr_t>(bufs), m->q8_bufs);
+    } else {
+        ALLOC(D.X, float*, kRows * d * 4, true)
+        ALLOC(D.A, void*, kRows * d * 4, true)
+        ALLOC(D.ssq, float*, (d / 16) * kRows * 4, true)
+        ALLOC(D.Q_hi, void*, kRows * q * 4, true)
+        ALLOC(D.Q_lo, void*, kRows * q * 4, true)
+        ALLOC(D.att_part, float*, att_part_bytes, true)
+        ALLOC(D.xch, float*, xch_bytes, true)
+        ALLOC(D.xch_ticket, int*, kSplitTickets * 4, true)
+        ALLOC(D.O, void*, kRows * q * 4, true)
+        ALLOC(D.H, void*, kRows * F * 4, true)
+    }
     ALLOC(D.logits, float*, kRows * V * 4, true)
-    ALLOC(D.best_val, float*, (size_t)m->nwg * kRows * 4, true)
-    ALLOC(D.best_idx, int*, (size_t)m->nwg * kRows * 4, true)
+    ALLOC(D.best_val, float*, best_bytes, true)
+    ALLOC(D.best_idx, int*, best_bytes, true)
 #undef ALLOC
     if (hipMemcpyAsync(const_cast<DevLayer*>(D.layers), m->layers_host.data(), sizeof(DevLayer) * c.n_layers,
                        hipMemcpyHostToDevice, m->stream) != hipSuccess)
@@ -731,18 +758,22 @@ int amusd_model_create(const amusd_config* cfg, void* hip_stream, amusd_model** 
             return p;
         };
         DevModel& S = m->dm_static;
-        S.X = static_cast<float*>(place(kRows * d * 4));
-        S.A = place(kRows * d * 4);
-        S.ssq = static_cast<float*>(place((d / 16) * kRows * 4));
-        S.Q_hi = place(kRows * q * 4);
-        S.Q_lo = place(kRows * q * 4);
-        S.att_part = static_cast<float*>(place(att_part_bytes));
-        S.xch = static_cast<float*>(place(xch_bytes));
-        S.xch_ticket = static_cast<int*>(place(kSplitTickets * 4));
-        S.O = place(kRows * q * 4);
-        S.H = place(kRows * F * 4);
-        S.best_val = static_cast<float*>(place((size_t)m->nwg * kRows * 4));
-        S.best_idx = static_cast<int*>(place((size_t)m->nwg * kRows * 4));
+        if (q8) {
+            off = q8_model_bufs(m->q8, D, kRows, reinterpret_cast<uintptr_t>(base), m->q8_static);
+        } else {
+            S.X = static_cast<float*>(place(kRows * d * 4));
+            S.A = place(kRows * d * 4);
+            S.ssq = static_cast<float*>(place((d / 16) * kRows * 4));
+            S.Q_hi = place(kRows * q * 4);
+            S.Q_lo = place(kRows * q * 4);
+            S.att_part = static_cast<float*>(place(att_part_bytes));
+            S.xch = static_cast<float*>(place(xch_bytes));
+            S.xch_ticket = static_cast<int*>(place(kSplitTickets * 4));
+            S.O = place(kRows * q * 4);
+            S.H = place(kRows * F * 4);
+        }
+        S.best_val = static_cast<float*>(place(best_bytes));
+        S.best_idx = static_cast<int*>(place(best_bytes));
         m->static_bytes = off;      // may exceed the array: amusd_verify_static then refuses the model
     }
     if (hipStreamSynchronize(m->stream) != hipSuccess) return bail(fail(AMUSD_E_HIP, "create: stream sync"));
@@ -792,6 +823,11 @@ int amusd_model_set_tensor(amusd_model* m, int32_t id, int32_t layer, const void
         }
         HIP_TRY(hipMemcpy(m->staging, data, bytes, hipMemcpyHostToDevice));
         src = m->staging;
+    }
+    if (m->q8) {
+        const int rc = q8_model_set(m->q8, id, layer, src, m->stream);
+        if (rc == AMUSD_OK) m->have[(size_t)id * (c.n_layers + 1) + slot] = 1;
+        return rc;
     }
     const int hd = c.head_dim;
     uint4* dst = nullptr;
@@ -871,6 +907,7 @@ int amusd_model_free(amusd_model* m) {
     if (!m) return AMUSD_OK;
     if (m->stream || !m->allocs.empty()) (void)hipStreamSynchronize(m->stream);
     for (void* p : m->allocs) (void)hipFree(p);
+    if (m->q8) q8_model_free(m->q8);
     if (m->staging) (void)hipFree(m->staging);
     if (m->hstage) (void)hipHostFree(m->hstage);
     if (m->export_host) (void)hipHostFree(m->export_host);
@@ -1145,15 +1182,15 @@ int amusd_stage_time(amusd_model* m, double* total_ms, int64_t* launches, int64_
     if (m->timer.stage < 0) return fail(AMUSD_E_STATE, "no stage selected for timing");
     const amusd_config& c = m->cfg;
     const int64_t d = c.d_model, q = (int64_t)c.n_q_heads * c.head_dim, kv = (int64_t)c.n_kv_heads * c.head_dim,
-                  F = c.d_ffn, V = c.vocab, e = m->esz();
+                  F = c.d_ffn, V = c.vocab;
     int64_t b = 0;
     switch (m->timer.stage) {
-        case AMUSD_STAGE_QKV: b = d * (q + 2 * kv) * e; break;
-        case AMUSD_STAGE_ATTENTION: b = 2 * kv * e * m->last_positions; break;
-        case AMUSD_STAGE_OPROJ: b = q * d * e; break;
-        case AMUSD_STAGE_GATEUP: b = 2 * d * F * e; break;
-        case AMUSD_STAGE_DOWN: b = d * F * e; break;
-        case AMUSD_STAGE_LMHEAD: b = V * d * e; break;
+        case AMUSD_STAGE_QKV: b = m->matrix_bytes(q + 2 * kv, d); break;
+        case AMUSD_STAGE_ATTENTION: b = 2 * c.n_kv_heads * m->position_bytes() * m->last_positions; break;
+        case AMUSD_STAGE_OPROJ: b = m->matrix_bytes(d, q); break;
+        case AMUSD_STAGE_GATEUP: b = m->matrix_bytes(2 * F, d); break;
+        case AMUSD_STAGE_DOWN: b = m->matrix_bytes(d, F); break;
+        case AMUSD_STAGE_LMHEAD: b = m->matrix_bytes(V, d); break;
         default: b = 0;
     }
     *total_ms = m->stage_ms;
@@ -1172,6 +1209,22 @@ int amusd_seq_get_kv(amusd_model* m, int32_t seq, int32_t layer, int32_t which, 
     const DevModel& D = m->dm;
     if (!out || layer < 0 || layer >= D.n_layers || (which != 0 && which != 1) || pos0 < 0 || n < 1 || pos0 + n > D.ctx_pad)
         return fail(AMUSD_E_ARG, "get_kv: bad argument");
+    if (m->q8) {
+        const size_t width = (size_t)D.Hkv * D.hd;
+        if (pos0 + n > D.max_ctx) return fail(AMUSD_E_ARG, "get_kv: bad argument");
+        std::vector<float> rows((size_t)n * width);
+        void* dev = nullptr;
+        HIP_TRY(dev_malloc(m->device, &dev, 2 * rows.size() * 4));
+        float* const kv = static_cast<float*>(dev);
+        hipError_t e = q8_model_read(m->q8, layer, seq, pos0, n, kv, kv + rows.size(), m->stream);
+        if (e == hipSuccess) e = hipStreamSynchronize(m->stream);
+        if (e == hipSuccess) e = hipMemcpy(rows.data(), kv + (which ? rows.size() : 0), rows.size() * 4, hipMemcpyDeviceToHost);
+        (void)hipFree(dev);
+        HIP_TRY(e);
+        for (int h = 0; h < D.Hkv; ++h)
+            for (int j = 0; j < n; ++j) std::memcpy(out + ((size_t)h * n + j) * D.hd, &rows[j * width + (size_t)h * D.hd], D.hd * 4);
+        return AMUSD_OK;
+    }
     const int esz = m->esz(), hd = D.hd, BK = m->block_keys(), EPL = 16 / esz;
     const size_t elems = (size_t)D.Hkv * D.ctx_pad * hd;
     std::vector<char> raw(elems * esz);
@@ -1206,14 +1259,14 @@ int64_t amusd_weight_bytes_per_pass(const amusd_model* m) {
     const amusd_config& c = m->cfg;
     const int64_t d = c.d_model, q = (int64_t)c.n_q_heads * c.head_dim, kv = (int64_t)c.n_kv_heads * c.head_dim,
                   F = c.d_ffn, V = c.vocab;
-    const int64_t per_layer = d * (q + 2 * kv) + q * d + 3 * d * F + 2 * d;
-    return (c.n_layers * per_layer + V * d + d) * m->esz();
+    const int64_t per_layer = m->matrix_bytes(q + 2 * kv, d) + m->matrix_bytes(d, q) + m->matrix_bytes(2 * F, d) + m->matrix_bytes(d, F) + 2 * d * m->esz();
+    return c.n_layers * per_layer + m->matrix_bytes(V, d) + d * m->esz();
 }
 
 int64_t amusd_kv_bytes_per_pass(const amusd_model* m, int32_t ctx_len, int32_t k) {
     if (!m) return fail(AMUSD_E_ARG, "null model");
     const amusd_config& c = m->cfg;
-    return (int64_t)c.n_layers * 2 * c.n_kv_heads * c.head_dim * m->esz() * ((int64_t)ctx_len + k);
+    return (int64_t)c.n_layers * 2 * c.n_kv_heads * m->position_bytes() * ((int64_t)ctx_len + k);
 }
 
 int amusd_calibration_copy(void* dst, const void* src, int64_t bytes, void* hip_stream) {

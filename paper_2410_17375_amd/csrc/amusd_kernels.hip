@@ -1389,6 +1389,11 @@ static hipError_t launch_pass_t(const DevModel& M, const DevLayer* Ls, PassArgs&
     return hipGetLastError();
 }
 
+hipError_t launch_accept(const DevModel& M, const PassArgs& P, hipStream_t stream) {
+    hipLaunchKernelGGL(k_accept, dim3(1 + export_wgs(P.export_bytes, kRows * 64)), dim3(kRows * 64), 0, stream, M, P);
+    return hipGetLastError();
+}
+
 hipError_t launch_pass(const DevModel& M, const DevLayer* Ls, PassArgs P, int nwg, hipStream_t stream, StageTimer* tm) {
     if (M.dtype)
         return M.hd == 128 ? launch_pass_t<BF16, 128>(M, Ls, P, nwg, stream, tm)

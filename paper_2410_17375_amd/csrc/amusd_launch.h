@@ -51,6 +51,9 @@ hipError_t launch_stream_chain(const uint4* buf, size_t buf_words, size_t words_
 hipError_t launch_pass(const DevModel& M, const DevLayer* layers_host, PassArgs P, int nwg, hipStream_t stream,
                        StageTimer* timer);
 
+// The end of a pass whose arg-max partials are there: acceptance, and logits on their way to the host.
+hipError_t launch_accept(const DevModel& M, const PassArgs& P, hipStream_t stream);
+
 // One prefill pass: P.n rows (tokens in T.tokens) appended at P.L0; greedy tokens of all rows to T.greedy.
 // tiles: [kPfStages].
 hipError_t launch_prefill(const DevModel& M, const DevLayer* layers_host, const PrefillBufs& T, const PfTileSet* tiles, const PrefillArgs& P,

@@ -9,7 +9,7 @@
 #include <stdint.h>
 
 #include "../../include/amusd.h"
-#include "amusd_dev.h"
+#include "amusd_launch.h"
 
 // Opaque handles of the C interface.
 struct amusd_q8_matrix {
@@ -62,11 +62,54 @@ hipError_t launch_q8_rows(const void* x, int dtype, int64_t ldx, const void* add
 hipError_t launch_q8_gemm(const amusd_q8_matrix& w, const int8_t* x, int64_t ldx, const float* scale, int rows, void* out, int dtype, int64_t ldo,
                           void* work, int64_t work_bytes, hipStream_t stream);
 int64_t q8_gemm_workspace(const amusd_q8_matrix& w, int rows);
+// Memory of the handles; the caller waits for the stream before it uses them.
+typedef hipError_t (*Q8Alloc)(int device, void** p, size_t bytes);
+hipError_t q8_matrix_take(amusd_q8_matrix& m, int n, int k, bool gated, Q8Alloc alloc, hipStream_t stream);
+hipError_t launch_q8_matrix(const amusd_q8_matrix& m, const void* w, int dtype, int64_t ld, const float* scale, int rows, int first, int part,
+                            hipStream_t stream);
+void q8_matrix_drop(amusd_q8_matrix& m);
+hipError_t q8_cache_take(amusd_q8_cache& c, int n_layers, int n_seqs, int n_q_heads, int n_kv_heads, int head_dim, int capacity, int block, Q8Alloc alloc,
+                         hipStream_t stream);
+void q8_cache_drop(amusd_q8_cache& c);
+void q8_append_units(Q8Segs& S);
 void q8_attention_plan(amusd_q8_cache& c);        // chunk, max_chunks and part_tiles from the sizes
 hipError_t launch_q8_append(const amusd_q8_cache& c, int layer, const Q8Segs& S, const void* k, const void* v, int64_t ld, const float* cos,
                             const float* sin, hipStream_t stream);
 hipError_t launch_q8_read(const amusd_q8_cache& c, int layer, const Q8Segs& S, void* k, void* v, int dtype, int64_t ld, hipStream_t stream);
 hipError_t launch_q8_attention(const amusd_q8_cache& c, int layer, const Q8Segs& S, const void* q, int64_t ldq, float scale, const float* cos,
                                const float* sin, void* out, int64_t ldo, hipStream_t stream);
+
+// ---- models in 8 bits (AMUSD_DTYPE_INT8): a pass is the operators above one after the other.  Weak: the host side links
+// without them where it is tested on its own, on a CPU.
+struct Q8Model;
+
+// Buffers of a pass of up to `cap` rows.
+struct Q8Bufs {
+    int cap = 0;
+    float* X;              // residual stream [cap][d]
+    int8_t* q;             // 8-bit rows on their way into a product
+    float* s;              // their scales
+    uint16_t* qkv;         // [cap][nqkv]
+    uint16_t* att;         // [cap][qdim]
+    uint16_t* delta;       // what a block adds to the residual stream [cap][d]
+    uint16_t* h;           // [cap][F]
+    void* work;            // of the products; zeros between passes
+    int64_t work_bytes;
+    float* logits;         // [min(cap, 128)][V], rows of a prompt whose arg-max alone is wanted; not in a pass of 16 rows
+};
+
+__attribute__((weak)) int q8_model_create(const DevModel& D, int device, Q8Alloc alloc, hipStream_t stream, Q8Model** out);
+__attribute__((weak)) void q8_model_free(Q8Model* q);
+// One tensor in bf16, on the device.
+__attribute__((weak)) int q8_model_set(Q8Model* q, int id, int layer, const void* src, hipStream_t stream);
+// Lays the buffers out from `base`; bytes.
+__attribute__((weak)) size_t q8_model_bufs(const Q8Model* q, const DevModel& D, int cap, uintptr_t base, Q8Bufs& B);
+__attribute__((weak)) hipError_t q8_model_pass(const Q8Model* q, const DevModel& D, const DevLayer* layers, const Q8Bufs& B, const PassArgs& P,
+                                               hipStream_t stream, StageTimer* timer);
+__attribute__((weak)) hipError_t q8_model_prefill(const Q8Model* q, const DevModel& D, const DevLayer* layers, const Q8Bufs& B, const PrefillBufs& T,
+                                                  const PrefillArgs& P, int tail, hipStream_t stream);
+// Rows of a layer's cache as fp32 rows on the device.
+__attribute__((weak)) hipError_t q8_model_read(const Q8Model* q, int layer, int seq, int pos0, int n, float* k, float* v, hipStream_t stream);
+constexpr int kQ8LmParts = 64;     // stretches of the vocabulary whose arg-max is found apart
 
 }  // namespace amusd

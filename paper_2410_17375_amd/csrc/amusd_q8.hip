@@ -381,51 +381,130 @@ hipError_t launch_q8_read(const amusd_q8_cache& c, int layer, const Q8Segs& S, v
 }
 
 // ---------------------------------------------------------------- weights to 8 bits, in operand order
-// One wave a feature: finds its scale (unless it is given), then writes the feature's bytes.
+// One wave a row of the source: finds its scale (unless it is given), then writes the feature's bytes.  Row i is feature first + i
+// of the matrix or, in a gated one, its gate's or up projection's (part 1, 2) feature i.
 template <class T>
 __global__ void __launch_bounds__(64) k_q8_matrix(uint4* __restrict__ frag, float* __restrict__ scale, const T* __restrict__ w, int64_t ld,
-                                                  const float* __restrict__ given, int n, int k, int gated) {
-    const int dst = blockIdx.x;                                  // destination feature, the padding's among them
-    const int tile = dst >> 4, r = dst & 15, lane = threadIdx.x;
-    const int col = gated ? (tile >> 1) * 16 + r : dst;
-    const bool real = col < n;
-    const int64_t src = gated ? (int64_t)(tile & 1) * n + col : col;
-    w += real ? src * ld : 0;
+                                                  const float* __restrict__ given, int k, int first, int part) {
+    const int i = blockIdx.x, lane = threadIdx.x;
+    const int tile = part ? (i >> 4) * 2 + part - 1 : (first + i) >> 4, r = part ? i & 15 : (first + i) & 15;
+    w += i * ld;
     double s = 0.;
-    bool bad = false;
+    auto value = [&](int c) {
+        if constexpr (sizeof(T) == 2) return bf16_to_f32(w[c]);
+        else return __uint_as_float(w[c]);
+    };
     if constexpr (sizeof(T) > 1) {
         float most = 0.f;
-        if (real)
-            for (int i = lane; i < k; i += 64) {
-                float x;
-                if constexpr (sizeof(T) == 2) x = bf16_to_f32(w[i]);
-                else x = __uint_as_float(w[i]);
-                bad |= !(fabsf(x) <= 3.402823466e38f);
-                most = fmaxf(most, fabsf(x));
-            }
+        bool bad = false;
+        for (int c = lane; c < k; c += 64) {
+            const float x = value(c);
+            bad |= !(fabsf(x) <= 3.402823466e38f);
+            most = fmaxf(most, fabsf(x));
+        }
         const double m = wave_max(bad ? INFINITY : (double)most);
         bad = !(m <= 3.402823466e38);
         s = bad ? 0. : (double)(float)(m / 127.);
-        if (lane == 0) scale[dst] = bad ? __uint_as_float(0x7FC00000u) : (float)s;
+        if (lane == 0) scale[tile * 16 + r] = bad ? __uint_as_float(0x7FC00000u) : (float)s;
     } else if (lane == 0) {
-        scale[dst] = real ? given[src] : 0.f;
+        scale[tile * 16 + r] = given[i];
     }
     const int kblocks = (k + 63) / 64;
     int8_t* out = reinterpret_cast<int8_t*>(frag);
     for (int kb = 0; kb < kblocks; ++kb) {
         const int c = kb * 64 + lane;
         int8_t b = 0;
-        if (real && c < k) {
-            if constexpr (sizeof(T) == 1) {
-                b = (int8_t)w[c];
-            } else {
-                float x;
-                if constexpr (sizeof(T) == 2) x = bf16_to_f32(w[c]);
-                else x = __uint_as_float(w[c]);
-                b = s > 0. ? (int8_t)(int)fmin(fmax(rint((double)x / s), -127.), 127.) : (int8_t)0;
-            }
+        if (c < k) {
+            if constexpr (sizeof(T) == 1) b = (int8_t)w[c];
+            else b = s > 0. ? (int8_t)(int)fmin(fmax(rint((double)value(c) / s), -127.), 127.) : (int8_t)0;
         }
         out[(((size_t)tile * kblocks + kb) * 64 + (lane >> 4) * 16 + r) * 16 + (lane & 15)] = b;
+    }
+}
+
+hipError_t launch_q8_matrix(const amusd_q8_matrix& m, const void* w, int dtype, int64_t ld, const float* scale, int rows, int first, int part,
+                            hipStream_t stream) {
+    auto go = [&](auto kernel, auto* src) {
+        hipLaunchKernelGGL(kernel, dim3(rows), dim3(64), 0, stream, const_cast<uint4*>(m.frag), const_cast<float*>(m.scale), src, ld, scale, m.k, first, part);
+    };
+    if (dtype == AMUSD_DTYPE_FP32) go(k_q8_matrix<uint32_t>, static_cast<const uint32_t*>(w));
+    else if (dtype == AMUSD_DTYPE_BF16) go(k_q8_matrix<uint16_t>, static_cast<const uint16_t*>(w));
+    else go(k_q8_matrix<int8_t>, static_cast<const int8_t*>(w));
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- handles
+hipError_t q8_device(int& device, int& cus) {
+    hipError_t e = hipGetDevice(&device);
+    if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device);
+    return e;
+}
+
+hipError_t q8_matrix_take(amusd_q8_matrix& m, int n, int k, bool gated, Q8Alloc alloc, hipStream_t stream) {
+    m.gated = gated;
+    m.n = gated ? n / 2 : n;
+    m.k = k;
+    m.kblocks = (k + 63) / 64;
+    m.tiles = (m.n + 15) / 16 * (gated ? 2 : 1);
+    void *frag = nullptr, *scale = nullptr;
+    const size_t bytes = (size_t)m.tiles * m.kblocks * 1024, scales = (size_t)m.tiles * 16 * 4;
+    hipError_t e = q8_device(m.device, m.cus);
+    if (e == hipSuccess) e = alloc(m.device, &frag, bytes);
+    m.frag = static_cast<const uint4*>(frag);
+    if (e == hipSuccess) e = alloc(m.device, &scale, scales);
+    m.scale = static_cast<const float*>(scale);
+    // (zeros are what pads features and columns)
+    if (e == hipSuccess) e = hipMemsetAsync(frag, 0, bytes, stream);
+    if (e == hipSuccess) e = hipMemsetAsync(scale, 0, scales, stream);
+    return e;
+}
+void q8_matrix_drop(amusd_q8_matrix& m) {
+    if (m.frag) (void)hipFree(const_cast<uint4*>(m.frag));
+    if (m.scale) (void)hipFree(const_cast<float*>(m.scale));
+    m.frag = nullptr;
+    m.scale = nullptr;
+}
+
+hipError_t q8_cache_take(amusd_q8_cache& c, int n_layers, int n_seqs, int n_q_heads, int n_kv_heads, int head_dim, int capacity, int block, Q8Alloc alloc,
+                         hipStream_t stream) {
+    c.n_layers = n_layers;
+    c.n_seqs = n_seqs;
+    c.Hq = n_q_heads;
+    c.Hkv = n_kv_heads;
+    c.hd = head_dim;
+    c.G = n_q_heads / n_kv_heads;
+    c.block = block;
+    c.cap = (capacity + kQ8Group - 1) / kQ8Group * kQ8Group;
+    hipError_t e = q8_device(c.device, c.cus);
+    q8_attention_plan(c);
+    const size_t heads = (size_t)n_layers * n_seqs * n_kv_heads, bytes = heads * c.cap * head_dim, scales = heads * (c.cap / block) * 4;
+    auto take = [&](auto& p, size_t n, bool zero) {
+        if (e != hipSuccess) return;
+        void* got = nullptr;
+        e = alloc(c.device, &got, n);
+        p = static_cast<std::remove_reference_t<decltype(p)>>(got);
+        if (e == hipSuccess && zero) e = hipMemsetAsync(got, 0, n, stream);
+    };
+    // zeros: positions that were never written take part in tiles, with weight 0
+    take(c.k, bytes, true);
+    take(c.v, bytes, true);
+    take(c.ks, scales, true);
+    take(c.vs, scales, true);
+    take(c.part, (size_t)c.part_tiles * c.max_chunks * (head_dim + 2) * 16 * 4, false);
+    return e;
+}
+void q8_cache_drop(amusd_q8_cache& c) {
+    for (void* p : {(void*)c.k, (void*)c.v, (void*)c.ks, (void*)c.vs, (void*)c.part})
+        if (p) (void)hipFree(p);
+    c.k = c.v = nullptr;
+    c.ks = c.vs = c.part = nullptr;
+}
+
+void q8_append_units(Q8Segs& S) {
+    S.units = 0;
+    for (int i = 0; i < S.n_seg; ++i) {
+        S.s[i].unit0 = S.units;
+        S.units += (S.s[i].pos0 + S.s[i].n - 1) / kQ8Group - S.s[i].pos0 / kQ8Group + 1;
     }
 }
 
@@ -440,6 +519,8 @@ namespace {
         hipError_t e_ = (expr);                                                                         \
         if (e_ != hipSuccess) return report(AMUSD_E_HIP, #expr, hipGetErrorString(e_));                 \
     } while (0)
+
+hipError_t q8_malloc(int, void** p, size_t bytes) { return hipMalloc(p, bytes); }
 
 bool float_dtype(int dtype) { return dtype == AMUSD_DTYPE_FP32 || dtype == AMUSD_DTYPE_BF16; }
 bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -524,46 +605,27 @@ int amusd_q8_matrix_create(const void* w, int32_t dtype, const float* scale, int
     if (n < 1 || k < 1 || ld < k || (gated && n % 2) || n > (1 << 28) || k > kQ8MaxK) return report(AMUSD_E_ARG, "q8_matrix: bad sizes");
     amusd_q8_matrix* m = new (std::nothrow) amusd_q8_matrix();
     if (!m) return report(AMUSD_E_NOMEM, "q8_matrix: handle");
-    m->gated = gated != 0;
-    m->n = gated ? n / 2 : n;
-    m->k = k;
-    m->kblocks = (k + 63) / 64;
-    m->tiles = (m->n + 15) / 16 * (gated ? 2 : 1);
     const size_t esz = dtype == AMUSD_DTYPE_FP32 ? 4 : dtype == AMUSD_DTYPE_BF16 ? 2 : 1;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    void *frag = nullptr, *sc = nullptr, *tmp = nullptr, *tmp_scale = nullptr;
-    hipError_t e = hipGetDevice(&m->device);
-    if (e == hipSuccess) e = hipDeviceGetAttribute(&m->cus, hipDeviceAttributeMultiprocessorCount, m->device);
-    if (e == hipSuccess) e = hipMalloc(&frag, (size_t)m->tiles * m->kblocks * 1024);
-    if (e == hipSuccess) e = hipMalloc(&sc, (size_t)m->tiles * 16 * 4);
-    const void* src = w;
-    const float* src_scale = scale;
+    hipError_t e = q8_matrix_take(*m, n, k, gated, q8_malloc, stream);
+    void *tmp = nullptr, *tmp_scale = nullptr;
     if (!on_device_) {
         const size_t bytes = ((size_t)(n - 1) * ld + k) * esz;
         if (e == hipSuccess) e = hipMalloc(&tmp, bytes);
         if (e == hipSuccess) e = hipMemcpy(tmp, w, bytes, hipMemcpyHostToDevice);
-        src = tmp;
+        w = tmp;
         if (scale) {
             if (e == hipSuccess) e = hipMalloc(&tmp_scale, (size_t)n * 4);
             if (e == hipSuccess) e = hipMemcpy(tmp_scale, scale, (size_t)n * 4, hipMemcpyHostToDevice);
-            src_scale = static_cast<const float*>(tmp_scale);
+            scale = static_cast<const float*>(tmp_scale);
         }
     }
-    if (e == hipSuccess) {
-        const dim3 grid(m->tiles * 16);
-        auto go = [&](auto kernel, auto p) {
-            hipLaunchKernelGGL(kernel, grid, dim3(64), 0, stream, static_cast<uint4*>(frag), static_cast<float*>(sc), p, ld, src_scale, m->n, k, m->gated);
-        };
-        if (esz == 4) go(k_q8_matrix<uint32_t>, static_cast<const uint32_t*>(src));
-        else if (esz == 2) go(k_q8_matrix<uint16_t>, static_cast<const uint16_t*>(src));
-        else go(k_q8_matrix<int8_t>, static_cast<const int8_t*>(src));
-        e = hipGetLastError();
-    }
+    if (e == hipSuccess) e = launch_q8_matrix(*m, w, dtype, ld, scale, m->n, 0, gated ? 1 : 0, stream);
+    if (e == hipSuccess && gated)
+        e = launch_q8_matrix(*m, static_cast<const char*>(w) + (size_t)m->n * ld * esz, dtype, ld, scale ? scale + m->n : nullptr, m->n, 0, 2, stream);
     if (e == hipSuccess) e = hipStreamSynchronize(stream);
     if (tmp) (void)hipFree(tmp);
     if (tmp_scale) (void)hipFree(tmp_scale);
-    m->frag = static_cast<const uint4*>(frag);
-    m->scale = static_cast<const float*>(sc);
     if (e != hipSuccess) {
         amusd_q8_matrix_free(m);
         return report(AMUSD_E_HIP, "q8_matrix", hipGetErrorString(e));
@@ -574,8 +636,7 @@ int amusd_q8_matrix_create(const void* w, int32_t dtype, const float* scale, int
 
 int amusd_q8_matrix_free(amusd_q8_matrix* m) {
     if (!m) return AMUSD_OK;
-    if (m->frag) (void)hipFree(const_cast<uint4*>(m->frag));
-    if (m->scale) (void)hipFree(const_cast<float*>(m->scale));
+    q8_matrix_drop(*m);
     delete m;
     return AMUSD_OK;
 }
@@ -610,32 +671,8 @@ int amusd_q8_cache_create(int32_t n_layers, int32_t n_seqs, int32_t n_q_heads, i
     if (n_q_heads % n_kv_heads || (G != 1 && G != 2 && G != 4 && G != 8)) return report(AMUSD_E_ARG, "q8_cache: n_q_heads / n_kv_heads must be 1, 2, 4 or 8");
     amusd_q8_cache* c = new (std::nothrow) amusd_q8_cache();
     if (!c) return report(AMUSD_E_NOMEM, "q8_cache: handle");
-    c->n_layers = n_layers;
-    c->n_seqs = n_seqs;
-    c->Hq = n_q_heads;
-    c->Hkv = n_kv_heads;
-    c->hd = head_dim;
-    c->G = G;
-    c->block = block;
-    c->cap = (capacity + kQ8Group - 1) / kQ8Group * kQ8Group;
-    hipError_t e = hipGetDevice(&c->device);
-    if (e == hipSuccess) e = hipDeviceGetAttribute(&c->cus, hipDeviceAttributeMultiprocessorCount, c->device);
-    q8_attention_plan(*c);
-    const size_t heads = (size_t)n_layers * n_seqs * n_kv_heads, bytes = heads * c->cap * head_dim, scales = heads * (c->cap / block) * 4;
     const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    auto take = [&](auto& p, size_t n, bool zero) {
-        if (e != hipSuccess) return;
-        void* got = nullptr;
-        e = hipMalloc(&got, n);
-        p = static_cast<std::remove_reference_t<decltype(p)>>(got);
-        if (e == hipSuccess && zero) e = hipMemsetAsync(got, 0, n, stream);
-    };
-    // zeros: positions that were never written take part in tiles, with weight 0
-    take(c->k, bytes, true);
-    take(c->v, bytes, true);
-    take(c->ks, scales, true);
-    take(c->vs, scales, true);
-    take(c->part, (size_t)c->part_tiles * c->max_chunks * (head_dim + 2) * 16 * 4, false);
+    hipError_t e = q8_cache_take(*c, n_layers, n_seqs, n_q_heads, n_kv_heads, head_dim, capacity, block, q8_malloc, stream);
     if (e == hipSuccess) e = hipStreamSynchronize(stream);
     if (e != hipSuccess) {
         amusd_q8_cache_free(c);
@@ -647,8 +684,7 @@ int amusd_q8_cache_create(int32_t n_layers, int32_t n_seqs, int32_t n_q_heads, i
 
 int amusd_q8_cache_free(amusd_q8_cache* c) {
     if (!c) return AMUSD_OK;
-    for (void* p : {(void*)c->k, (void*)c->v, (void*)c->ks, (void*)c->vs, (void*)c->part})
-        if (p) (void)hipFree(p);
+    q8_cache_drop(*c);
     delete c;
     return AMUSD_OK;
 }
@@ -659,11 +695,7 @@ int amusd_q8_cache_append(amusd_q8_cache* c, int32_t layer, int32_t n_seq, const
     int rc = segments(c, layer, n_seq, seq_ids, pos0, n, S);
     if (rc || (rc = rope_args(rope_cos, rope_sin))) return rc;
     if (!k || !v || ld < (int64_t)c->Hkv * c->hd || !aligned(k, 2) || !aligned(v, 2)) return report(AMUSD_E_ARG, "q8_cache_append: bad rows");
-    S.units = 0;
-    for (int i = 0; i < n_seq; ++i) {
-        S.s[i].unit0 = S.units;
-        S.units += (pos0[i] + n[i] - 1) / kQ8Group - pos0[i] / kQ8Group + 1;
-    }
+    q8_append_units(S);
     Q8_TRY(launch_q8_append(*c, layer, S, k, v, ld, rope_cos, rope_sin, static_cast<hipStream_t>(hip_stream)));
     return AMUSD_OK;
 }

@@ -57,4 +57,46 @@ inline bool attention_packs_rows(bool bf16, int head_dim, int group, int units, 
     return bf16 && head_dim == 64 && run_blocks < 8;
 }
 
+// Products of 8-bit integers: forms for few rows, whose workgroups' eight waves split the contraction of MT x 16 rows and NT x 16 features
+// (kQ8FewMTxNT), and for many, whose workgroups hold a tile of the result (kQ8Tile<features>x<rows>).
+enum Q8Form { kQ8Few1x1, kQ8Few1x2, kQ8Few2x1, kQ8Few2x2, kQ8Few2x4, kQ8Few4x4, kQ8Tile64, kQ8Tile128x64, kQ8Tile128, kQ8Tile256 };
+
+// Which: up to 16 rows by the number of feature tiles alone (one a workgroup while there is a compute unit for each; us with 1x1 / 1x2, 8
+// rows: 4096 x 4096 5.3 / 6.0, 6144 features 7.6 / 6.8, 28672 24.9 / 19.8); with more rows by an estimate of each form's time, us:
+//   few: 3 + a compute unit's rounds x blocks of 64 columns x (0.020 a feature tile + 0.022 a row tile): what a compute unit loads at
+//     about 50 GB/s;
+//   tiles: a block takes its workgroup at least `alone` (the loads' latency); where compute units are full, `full` a workgroup of them.
+//     256 x 256 has a compute unit to itself: rounds x (blocks x 0.55 to 0.70 + 9); clocks fall as more of the chip multiplies.
+// Measured (MI355X, 8B and 1B projections, 17 to 2048 rows; the estimate's choice / the best): 2048 rows gate/up 209 / 209, QKV 53 / 53,
+// O-projection 37.5 / 37.5, down 122 / 122; 128 rows gate/up 33.5 / 33.5, O-projection 10.3 / 10.3; 64 rows gate/up 27.5 / 27.5, down 23 / 23.
+inline Q8Form q8_gemm_form(int tiles, int kblocks, bool gated, int rows, int cus) {
+    if (rows <= 16) return !gated && tiles <= cus ? kQ8Few1x1 : kQ8Few1x2;
+    const double chip = cus / 256., kb = kblocks;
+    Q8Form best = kQ8Few2x2;
+    double least = 1e30;
+    auto offer = [&](Q8Form f, double us) {
+        if (us < least) { least = us; best = f; }
+    };
+    auto ceil_div = [](int a, int b) { return (a + b - 1) / b; };
+    auto few = [&](Q8Form f, int mt, int nt) {
+        const int wgs = ceil_div(tiles, nt) * ceil_div(rows, 16 * mt);
+        offer(f, 3 + ceil_div(wgs, cus) * kb * (0.020 * nt + 0.022 * mt));
+    };
+    if (!gated) few(kQ8Few2x1, 2, 1);
+    few(kQ8Few2x2, 2, 2);
+    few(kQ8Few2x4, 2, 4);
+    few(kQ8Few4x4, 4, 4);
+    auto tile = [&](Q8Form f, int cols, int rows_of, double alone, double full) {
+        const int wgs = ceil_div(tiles, cols) * ceil_div(rows, rows_of);
+        const double shared = wgs * kb * full / 256 / chip;
+        offer(f, 4 + (kb * alone > shared ? kb * alone : shared));
+    };
+    tile(kQ8Tile64, 4, 64, 0.25, 0.128);
+    tile(kQ8Tile128x64, 8, 64, 0.29, 0.198);
+    tile(kQ8Tile128, 8, 128, 0.33, 0.28);
+    const int wgs = ceil_div(tiles, 16) * ceil_div(rows, 256), rounds = ceil_div(wgs, cus);
+    offer(kQ8Tile256, 3 + rounds * (kb * (0.55 + 0.15 * (wgs < cus ? (double)wgs / cus : 1.)) + 9));
+    return best;
+}
+
 }  // namespace amusd

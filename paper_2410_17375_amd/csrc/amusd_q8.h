@@ -10,6 +10,7 @@
 
 #include "../../include/amusd.h"
 #include "amusd_launch.h"
+#include "amusd_plan.h"
 
 // Opaque handles of the C interface.
 struct amusd_q8_matrix {

@@ -17,7 +17,12 @@ __device__ __forceinline__ v4i mfma_i8(uint4 a, uint4 b, v4i c) {
 // What every form of the product makes of a sum, in this order: a row's bits do not depend on the form.
 __device__ __forceinline__ float q8_value(int sum, float sx, float sw) { return (float)sum * sx * sw; }
 __device__ __forceinline__ void q8_put(float* p, float v) { *p = v; }
-__device__ __forceinline__ void q8_put(uint16_t* p, float v) { *p = (uint16_t)(v == v ? bf16_rne(v) : 0x7FC0u); }
+__device__ __forceinline__ void q8_put(uint16_t* p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
+// silu(gate) * up.  With the instructions for 2^x and 1/x (an error of one unit in the last place each): a division in full is ten
+// instructions more for each of the outputs, which wait for nothing else.
+__device__ __forceinline__ float q8_swiglu(float gate, float up) {
+    return gate * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(gate * -1.44269504f)) * up;
+}
 
 // Few rows: the weights are read once and their bytes bound it.  A workgroup owns NT tiles of 16 features, its waves every
 // eighth block of 64 columns, and each wave keeps D blocks under way; the sums meet in LDS.  MT: tiles of 16 rows.
@@ -94,7 +99,7 @@ __global__ void __launch_bounds__(512) k_q8_gemm_rows(const uint4* __restrict__ 
         float v;
         if constexpr (GATED) {
             const float* s = wscale + (tile0 + 2 * t) * 16 + (f & 15);
-            v = swiglu(q8_value(sum(m, 2 * t, at), sx, s[0]), q8_value(sum(m, 2 * t + 1, at), sx, s[16]));
+            v = q8_swiglu(q8_value(sum(m, 2 * t, at), sx, s[0]), q8_value(sum(m, 2 * t + 1, at), sx, s[16]));
         } else {
             v = q8_value(sum(m, t, at), sx, wscale[gc]);
         }
@@ -102,25 +107,226 @@ __global__ void __launch_bounds__(512) k_q8_gemm_rows(const uint4* __restrict__ 
     }
 }
 
+// Many rows: the matrix instructions bound it.  A workgroup of WN x WM waves has WN * A tiles of 16 features x WM * B tiles of 16 rows,
+// a wave A x B of them.  Both operands go through rings in LDS, filled by loads that deliver straight into it:
+//   weights a block of 64 columns at a time, as they lie in memory (4 slots);
+//   rows two blocks at a time (3 slots), a load fetching 8 whole lines of 128 bytes: with 16 half lines a load, a block of 256 x 256 took
+//   0.75 us instead of 0.56.  The eight 16-byte pieces of a line lie in an order that depends on the row, so that the 16
+//   lanes that read a column of pieces find them in different banks.
+template <int WN_, int WM_, int A_, int B_, int WAVES_>
+struct Q8Shape {
+    static constexpr int WN = WN_, WM = WM_, A = A_, B = B_, kMinWaves = WAVES_;
+    static constexpr int kWavesOf = WN * WM, kThreads = kWavesOf * 64;
+    static constexpr int kColTiles = WN * A, kRowTiles = WM * B;
+    static constexpr int NW = kColTiles / kWavesOf, NX = kRowTiles / kWavesOf;      // loads of a wave and block
+    static constexpr int kWSlots = 4, kXSlots = 3, kWBytes = kColTiles * 1024, kXBytes = kRowTiles * 2048;
+    static constexpr int kLds = kWSlots * kWBytes + kXSlots * kXBytes;
+    static_assert(kColTiles % kWavesOf == 0 && kRowTiles % kWavesOf == 0 && A % 2 == 0, "");
+};
+
+template <class Sh, class OUT, bool GATED>
+__global__ void __launch_bounds__(Sh::kThreads, Sh::kMinWaves) k_q8_gemm_tile(const uint4* __restrict__ frag, const float* __restrict__ wscale, int kblocks,
+                                                                             int k, int tiles, int n, const int8_t* __restrict__ x, int64_t ldx,
+                                                                             const float* __restrict__ xscale, int rows, OUT* __restrict__ out, int64_t ldo,
+                                                                             int row_wgs, int wgs) {
+    constexpr int WN = Sh::WN, A = Sh::A, B = Sh::B, NW = Sh::NW, NX = Sh::NX, NPW = NW + NX, MID = A / 2, WR = A >= 4 ? 4 : 2, WD = WR / 2;
+    static_assert(MID + WD <= A && A % WR == 0, "");
+    extern __shared__ char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
+    const int wn = wave % WN, wm = wave / WN;
+    // Workgroups are dealt to the 8 XCDs in turn: each gets a run of neighbouring tiles, rows fastest, so that the weights that its
+    // workgroups want at a time are few and in its L2.
+    const int xcd = blockIdx.x & 7, per = wgs >> 3, more = wgs & 7;
+    const int at = xcd * per + min(xcd, more) + (blockIdx.x >> 3);
+    const int row0 = at % row_wgs * (Sh::kRowTiles * 16), tile0 = at / row_wgs * Sh::kColTiles;
+    const char* wsrc[NW];
+#pragma unroll
+    for (int q = 0; q < NW; ++q) wsrc[q] = reinterpret_cast<const char*>(frag + (size_t)min(tile0 + wave * NW + q, tiles - 1) * kblocks * 64);
+    // rows: load q of half h of a pair of blocks is of the 8 rows from 8 * (h * kRowTiles + wave * NX + q)
+    const char* xsrc = reinterpret_cast<const char*>(x + (int64_t)row0 * ldx);
+    unsigned xoff[2][NX], xcol[2][NX];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int q = 0; q < NX; ++q) {
+            const int piece = h * Sh::kRowTiles + wave * NX + q;
+            xoff[h][q] = (unsigned)(min(piece * 8 + (lane >> 3), rows - 1 - row0) * ldx);
+            xcol[h][q] = ((lane & 7) ^ (lane >> 3) ^ (piece & 1)) * 16;
+        }
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)smem;
+    const unsigned ldsx = lds0 + Sh::kWSlots * Sh::kWBytes;
+    const int pairs = (kblocks + 1) / 2;
+    // Issues load q of NPW with block `b` of weights and half h of pair `p` of rows (past the end: the last once more, unused).
+    int wslot = 0, xslot = 0;
+    unsigned wdst = 0, wat = 0;
+    auto begin_w = [&](int b) {
+        wdst = lds0 + wslot * Sh::kWBytes + wave * (NW * 1024);
+        wat = (unsigned)min(b, kblocks - 1) * 1024u + lane * 16;
+        wslot = (wslot + 1) & 3;
+    };
+    auto load_w = [&](int q) { load_to_lds(wsrc[q], wat, wdst + q * 1024); };
+    auto load_x = [&](int q, int p, int h) {
+        const unsigned c = (unsigned)min(p, pairs - 1) * 128u + xcol[h][q];
+        load_to_lds(xsrc, xoff[h][q] + (c < (unsigned)k ? c : 0u), ldsx + xslot * Sh::kXBytes + (h * Sh::kRowTiles + wave * NX + q) * 1024);   // columns past k meet zeros
+    };
+    auto next_x = [&] { xslot = xslot == 2 ? 0 : xslot + 1; };
+    auto w_frag = [&](const char* slot, int f) { return *reinterpret_cast<const uint4*>(slot + f * 1024 + lane * 16); };
+    const int xread = (r >> 3) * 1024 + (r & 7) * 128 + ((g ^ (r & 7) ^ (r >> 3)) * 16);
+    auto x_frag = [&](const char* slot, int half, int f) { return *reinterpret_cast<const uint4*>(slot + f * 2048 + (half ? xread ^ 64 : xread)); };
+    const char* const wring = smem;
+    const char* const xring = smem + Sh::kWSlots * Sh::kWBytes;
+    v4i acc[A][B] = {};
+    uint4 wf[WR], xf[2][B];
+    // Before the loop: blocks 0 to 2 of the weights, pairs 0 and 1 of the rows; what the loop's first half block issues is left out.
+    constexpr int kFirst = NPW * (A - MID) / A;
+    begin_w(0);
+#pragma unroll
+    for (int q = 0; q < NW; ++q) load_w(q);
+#pragma unroll
+    for (int q = 0; q < 2 * NX; ++q) load_x(q % NX, 0, q / NX);
+    next_x();
+    begin_w(1);
+#pragma unroll
+    for (int q = 0; q < NW; ++q) load_w(q);
+#pragma unroll
+    for (int q = 0; q < NX; ++q) load_x(q, 1, 0);
+    begin_w(2);
+#pragma unroll
+    for (int q = 0; q < kFirst; ++q) {
+        if (q < NW) load_w(q);
+        else load_x(q - NW, 1, 1);
+    }
+    wait_vm<NPW + kFirst>();
+    __builtin_amdgcn_s_waitcnt(0xC07F);                  // lgkmcnt(0): no scalar load is pending in the loop
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < WD; ++i) wf[i] = w_frag(wring, wn * A + i);
+#pragma unroll
+    for (int j = 0; j < B; ++j) xf[0][j] = x_frag(xring, 0, wm * B + j);
+    int cw = 0, cx = 0, kb = 0;
+    // One block, its rows' fragments in xf[P] (P: which of its pair).  The next block is in LDS after the barrier in the middle, and the loads
+    // of what is three blocks ahead begin, into slots that every wave is past, a few with each tile's products.  Fragments are
+    // read from LDS well before their use: weights WD tiles ahead, rows half a block.
+    auto block = [&](auto parity) {
+        constexpr int P = decltype(parity)::value;
+        const char* cur = wring + cw * Sh::kWBytes;
+        cw = (cw + 1) & 3;
+        const char* nxt = wring + cw * Sh::kWBytes;
+        if (P) cx = cx == 2 ? 0 : cx + 1;
+        const char* nx = xring + cx * Sh::kXBytes;       // where the next block's rows are
+#pragma unroll
+        for (int i = 0; i < A; ++i) {
+            if (i == MID) {
+                wait_vm<NPW>();
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                begin_w(kb + 3);
+                if (!P) next_x();
+            }
+            // steps from the middle on fetch for (kb + 3, half P of pair kb / 2 + 2), those before it what the block before began
+            const int step = (i - MID + A) % A;
+#pragma unroll
+            for (int q = step * NPW / A; q < (step + 1) * NPW / A; ++q) {
+                if (q < NW) load_w(q);
+                else if (i >= MID) load_x(q - NW, (kb >> 1) + 2, P);
+                else load_x(q - NW, ((kb - 1) >> 1) + 2, 1 - P);
+            }
+            wf[(i + WD) % WR] = i + WD < A ? w_frag(cur, wn * A + i + WD) : w_frag(nxt, wn * A + i + WD - A);
+            if (i >= MID)
+#pragma unroll
+                for (int j = (i - MID) * B / (A - MID); j < (i - MID + 1) * B / (A - MID); ++j) xf[1 - P][j] = x_frag(nx, 1 - P, wm * B + j);
+#pragma unroll
+            for (int j = 0; j < B; ++j) acc[i][j] = mfma_i8(wf[i % WR], xf[P][j], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        ++kb;
+    };
+#pragma unroll 1
+    while (kb + 2 <= kblocks) {
+        block(std::integral_constant<int, 0>{});
+        block(std::integral_constant<int, 1>{});
+    }
+    if (kb < kblocks) block(std::integral_constant<int, 0>{});
+    wait_vm<0>();                                        // what was loaded past the end
+    // Lane: row r of a row tile, features 4 g .. 4 g + 3 of a feature tile.  Through LDS, so that whole lines are stored: a wave's rows
+    // at a distance of W elements, a little more than they have (banks).
+    __syncthreads();
+    constexpr int kOutTiles = GATED ? A / 2 : A, W = kOutTiles * 16 + 16 / (int)sizeof(OUT);
+    constexpr int kSpan = kOutTiles * 16 * (int)sizeof(OUT) / 16;             // 16-byte pieces of a row
+    OUT* const stage = reinterpret_cast<OUT*>(smem) + wave * (16 * W);
+    static_assert(Sh::kWavesOf * 16 * W * (int)sizeof(OUT) <= Sh::kLds, "");
+    const int col0 = (GATED ? (tile0 + wn * A) / 2 : tile0 + wn * A) * 16;
+    v4f sw[A];
+#pragma unroll
+    for (int i = 0; i < A; ++i) sw[i] = *reinterpret_cast<const v4f*>(wscale + min(tile0 + wn * A + i, tiles - 1) * 16 + g * 4);
+#pragma unroll
+    for (int j = 0; j < B; ++j) {
+        const int jrow = row0 + (wm * B + j) * 16;
+        const float sx = xscale[min(jrow + r, rows - 1)];
+#pragma unroll
+        for (int i = 0; i < A; i += GATED ? 2 : 1) {
+            OUT v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (GATED) q8_put(&v[e], q8_swiglu(q8_value(acc[i][j][e], sx, sw[i][e]), q8_value(acc[i + 1][j][e], sx, sw[i + 1][e])));
+                else q8_put(&v[e], q8_value(acc[i][j][e], sx, sw[i][e]));
+            }
+            __builtin_memcpy(stage + r * W + (GATED ? i / 2 : i) * 16 + g * 4, v, sizeof v);
+        }
+        __builtin_amdgcn_wave_barrier();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int c = lane; c < 16 * kSpan; c += 64) {
+            constexpr int kPiece = 16 / (int)sizeof(OUT);
+            const int row = jrow + c / kSpan, col = col0 + c % kSpan * kPiece;
+            OUT v[kPiece];
+            __builtin_memcpy(v, stage + c / kSpan * W + c % kSpan * kPiece, 16);
+            if (row >= rows || col >= n) continue;
+            OUT* o = out + (int64_t)row * ldo + col;
+            if (col + kPiece <= n) {
+                __builtin_memcpy(o, v, 16);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kPiece; ++e)
+                    if (col + e < n) o[e] = v[e];
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+}
+
 int64_t q8_gemm_workspace(const amusd_q8_matrix&, int) { return 0; }
 
 template <class OUT, bool GATED>
 static void gemm(const amusd_q8_matrix& w, const int8_t* x, int64_t ldx, const float* scale, int rows, OUT* out, int64_t ldo, hipStream_t stream) {
-    auto go = [&](auto kernel, int mt, int nt) {
+    auto few = [&](auto kernel, int mt, int nt) {
         const int lds = 8 * mt * nt * 256 * 4;
         (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         hipLaunchKernelGGL(kernel, dim3((w.tiles + nt - 1) / nt, (rows + mt * 16 - 1) / (mt * 16)), dim3(512), lds, stream, w.frag, w.scale, w.kblocks, w.k,
                            w.tiles, w.n, x, ldx, scale, rows, out, ldo);
     };
-    if (rows <= 16) {
-        if constexpr (!GATED) {
-            if (w.tiles <= w.cus) return go(k_q8_gemm_rows<OUT, GATED, 1, 1, 8>, 1, 1);
-        }
-        if (w.tiles <= 4 * w.cus) return go(k_q8_gemm_rows<OUT, GATED, 1, 2, 4>, 1, 2);
-        return go(k_q8_gemm_rows<OUT, GATED, 1, 4, 4>, 1, 4);
+    auto many = [&](auto shape) {
+        using Sh = decltype(shape);
+        const auto kernel = k_q8_gemm_tile<Sh, OUT, GATED>;
+        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Sh::kLds);
+        const int row_wgs = (rows + Sh::kRowTiles * 16 - 1) / (Sh::kRowTiles * 16), wgs = row_wgs * ((w.tiles + Sh::kColTiles - 1) / Sh::kColTiles);
+        hipLaunchKernelGGL(kernel, dim3(wgs), dim3(Sh::kThreads), Sh::kLds, stream, w.frag, w.scale, w.kblocks, w.k, w.tiles, w.n, x, ldx, scale, rows, out,
+                           ldo, row_wgs, wgs);
+    };
+    switch (q8_gemm_form(w.tiles, w.kblocks, w.gated, rows, w.cus)) {
+        case kQ8Few1x1: if constexpr (!GATED) return few(k_q8_gemm_rows<OUT, GATED, 1, 1, 4>, 1, 1); else return;
+        case kQ8Few1x2: return few(k_q8_gemm_rows<OUT, GATED, 1, 2, 4>, 1, 2);
+        case kQ8Few2x1: if constexpr (!GATED) return few(k_q8_gemm_rows<OUT, GATED, 2, 1, 8>, 2, 1); else return;
+        case kQ8Few2x2: return few(k_q8_gemm_rows<OUT, GATED, 2, 2, 4>, 2, 2);
+        case kQ8Few2x4: return few(k_q8_gemm_rows<OUT, GATED, 2, 4, 4>, 2, 4);
+        case kQ8Few4x4: return few(k_q8_gemm_rows<OUT, GATED, 4, 4, 2>, 4, 4);
+        case kQ8Tile64: return many(Q8Shape<2, 2, 2, 2, 4>{});
+        case kQ8Tile128x64: return many(Q8Shape<2, 2, 4, 2, 2>{});
+        case kQ8Tile128: return many(Q8Shape<2, 2, 4, 4, 2>{});
+        case kQ8Tile256: return many(Q8Shape<2, 4, 8, 4, 2>{});
     }
-    if (rows <= 32) return go(k_q8_gemm_rows<OUT, GATED, 2, 2, 4>, 2, 2);
-    go(k_q8_gemm_rows<OUT, GATED, 4, 2, 4>, 4, 2);
 }
 
 hipError_t launch_q8_gemm(const amusd_q8_matrix& w, const int8_t* x, int64_t ldx, const float* scale, int rows, void* out, int dtype, int64_t ldo,

@@ -25,8 +25,8 @@ struct amusd_q8_cache {
     int n_layers = 0, n_seqs = 0, Hq = 0, Hkv = 0, hd = 0, G = 0, cap = 0, block = 1, device = 0, cus = 0;
     int chunk = 0;                 // keys of a chunk: its sums are complete before they are merged
     int max_chunks = 0, part_tiles = 0;
-    int8_t* k = nullptr;           // [layer][seq][kv head][cap][hd]
-    int8_t* v = nullptr;           // [layer][seq][kv head][cap/32][hd/32][64 lanes][16]: operand order (q8_v_index)
+    int8_t* k = nullptr;           // [layer][seq][kv head][cap/16][hd/64][64 lanes][16]: operand order (q8_k_index)
+    int8_t* v = nullptr;           // [layer][seq][kv head][cap/32][hd/32][64 lanes][16]: q + 128 in operand order (q8_v_index)
     float* ks = nullptr;           // [layer][seq][kv head][cap/block]
     float* vs = nullptr;
     float* part = nullptr;         // [part_tiles][max_chunks][hd + 2][16]: numerators, reference, denominator of 16 pairs
@@ -51,7 +51,11 @@ struct Q8Segs {
     Q8Seg s[kMaxSegs];
 };
 
-// Byte of (position, column) in a kv head's values.  The 8 keys of a lane are those whose scores the lane holds: the weights then
+// Byte of (position, column) in a kv head's keys.
+__host__ __device__ inline size_t q8_k_index(int hd, int pos, int c) {
+    return (((size_t)(pos >> 4) * (hd >> 6) + (c >> 6)) * 64 + ((c & 63) >> 4) * 16 + (pos & 15)) * 16 + (c & 15);
+}
+// .. in its values.  The 8 keys of a lane are those whose scores the lane holds: the weights then
 // are the matrix instruction's operand as they come.
 __host__ __device__ inline size_t q8_v_index(int hd, int pos, int c) {
     return (((size_t)(pos >> 5) * (hd >> 5) + (c >> 5)) * 64 + ((pos & 15) >> 2) * 16 + (c & 15)) * 16 + ((c >> 4) & 1) * 8 + ((pos >> 4) & 1) * 4 +

@@ -293,22 +293,24 @@ __global__ void __launch_bounds__(256) k_q8_append(amusd_q8_cache C, int layer, 
     __syncthreads();
     // 4 bytes a thread: keys 4 columns of a position, values 4 positions of a column
     int8_t* out = (values ? C.v : C.k) + kvh * ((size_t)C.cap * HD);
+    // (values are kept as q + 128: amusd_q8_attention.hip)
+    const uint8_t bias = values ? 0x80 : 0;
     auto eight = [&](int r, int c, bool& write, int8_t old) {        // position p0 + r, column c
         const int pos = p0 + r, b = r / B;
         const float s = new_scale[b];
         if (pos >= from && pos < to) {
             write = true;
-            return (int8_t)(s > 0.f ? (int)fminf(fmaxf(rintf(rows[r][c] / s), -127.f), 127.f) : 0);
+            return (int8_t)((s > 0.f ? (int)fminf(fmaxf(rintf(rows[r][c] / s), -127.f), 127.f) : 0) ^ bias);
         }
         // held before, in a block whose scale has grown (from a block that this call does not touch `ratio` is 1)
         write = pos < from && pos < seg.pos0 && ratio[b] != 1.f;
-        return write ? (int8_t)(int)rintf((float)old * ratio[b]) : old;
+        return write ? (int8_t)((int)rintf((float)(int8_t)(old ^ bias) * ratio[b]) ^ bias) : old;
     };
     const int first_row = max(0, from / B * B - p0), last_row = to - p0;          // rows that can change
     if (!values) {
         for (int i = t; i < (last_row - first_row) * (HD / 4); i += 256) {
             const int r = first_row + i / (HD / 4), c = i % (HD / 4) * 4;
-            int8_t* p = out + (size_t)(p0 + r) * HD + c;
+            int8_t* p = out + q8_k_index(HD, p0 + r, c);
             const char4 old = *reinterpret_cast<const char4*>(p);
             bool w = false;
             char4 b;
@@ -364,7 +366,7 @@ __global__ void __launch_bounds__(256) k_q8_read(amusd_q8_cache C, int layer, Q8
         const int8_t* p = (values ? C.v : C.k) + kvh * ((size_t)C.cap * C.hd);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float y = (float)(values ? p[q8_v_index(C.hd, pos, c + e)] : p[(size_t)pos * C.hd + c + e]) * s;
+            const float y = (float)(values ? (int8_t)(p[q8_v_index(C.hd, pos, c + e)] ^ 0x80) : p[q8_k_index(C.hd, pos, c + e)]) * s;
             if constexpr (sizeof(T) == 2) out[x * 4 + e] = (T)(y == y ? bf16_rne(y) : 0x7FC0u);
             else out[x * 4 + e] = __float_as_uint(y);
         }

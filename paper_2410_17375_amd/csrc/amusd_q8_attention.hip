@@ -39,9 +39,8 @@ struct Q8Query {                                 // a launch's constants
 template <int HD>
 struct Tile {
     uint4 hi[HD / 64], lo[HD / 64];
-    float qs;                                    // score per unit of the integer product, without the key's scale
+    float qs;                                    // score (in units of log2) per unit of the integer product, without the key's scale; positive
     int pos;                                     // the pair's row's position (the last key that it sees); -1: no pair
-    int row, head;
 };
 
 template <int HD>
@@ -50,11 +49,9 @@ __device__ __forceinline__ Tile<HD> load_tile(const amusd_q8_cache& C, const Q8Q
     const int lane = threadIdx.x & 63, g = lane >> 4;
     const int p = tile * 16 + (lane & 15), pairs = seg.n * C.G;
     const int pc = min(p, pairs - 1);
-    T.row = pc / C.G;
-    T.head = kvh * C.G + pc % C.G;
-    const int pos = seg.pos0 + T.row;
+    const int row = pc / C.G, pos = seg.pos0 + row;
     T.pos = p < pairs ? pos : -1;
-    const uint16_t* src = Q.q + (int64_t)(seg.row0 + T.row) * Q.ldq + (int64_t)T.head * HD;
+    const uint16_t* src = Q.q + (int64_t)(seg.row0 + row) * Q.ldq + (int64_t)(kvh * C.G + pc % C.G) * HD;
     float x[HD / 64][16];
 #pragma unroll
     for (int f = 0; f < HD / 64; ++f) {
@@ -94,7 +91,7 @@ __device__ __forceinline__ Tile<HD> load_tile(const amusd_q8_cache& C, const Q8Q
     const bool bad = most >= 0x7F800000u;
     const float m = bad ? 0.f : __uint_as_float(most);
     const float inv = m > 0.f ? (float)kPlane / m : 0.f;
-    T.qs = bad ? __uint_as_float(0x7FC00000u) : m / (float)kPlane * Q.scale2;
+    T.qs = bad ? __uint_as_float(0x7FC00000u) : fmaxf(m / (float)kPlane * Q.scale2, 1.17549435e-38f);     // (not 0: 0 times -infinity)
 #pragma unroll
     for (int f = 0; f < HD / 64; ++f) {
         uint32_t hi[4] = {}, lo[4] = {};
@@ -113,138 +110,144 @@ __device__ __forceinline__ Tile<HD> load_tile(const amusd_q8_cache& C, const Q8Q
 
 __device__ __forceinline__ float pow2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Four signed bytes as half values: 1024 + (b + 128) is the half whose low byte is b + 128.
-__device__ __forceinline__ void bytes_to_half(uint32_t b, uint32_t& lo, uint32_t& hi) {
-    const uint32_t u = b ^ 0x80808080u;
-    const h2 off = {(_Float16)-1152.f, (_Float16)-1152.f};
-    lo = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + off);
-    hi = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + off);
+// Four bytes of values, which are kept as v + 128, as the halves 1152 + v: 1024 + u is the half whose low byte is u.  What the 1152 add
+// to the sums is taken off again at a chunk's end, with the sum of the weights that one more matrix instruction gives: a
+// third of the instructions of a subtraction for every value, and the sums, ten times larger so, are rounded a thousand times finer than
+// the values themselves were.
+__device__ __forceinline__ void bytes_to_half(uint32_t u, uint32_t& lo, uint32_t& hi) {
+    lo = __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u);
+    hi = __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u);
 }
 
 // A chunk's sums for 16 pairs: lane l has columns dt * 16 + 4 * (l / 16) + e of pair l % 16.
 template <int HD>
 struct Sums {
-    v4f acc[HD / 16];
+    v4f acc[HD / 16], weights;                   // weights: their sum (as scaled for the product), the same in all four
     float ref, den;
 };
 
-// Scales of the 4 keys pos .. pos + 3 (pos a multiple of 4).
+// Scales of a chunk's keys and values, 8 keys a lane: two loads of the wave have those of a longest chunk.
+constexpr int kMaxChunk = 512;
+struct Scales {
+    v4f k[2], v[2];
+};
 template <bool PER_TOKEN>
-__device__ __forceinline__ v4f key_scales(const float* s, int pos, int shift) {
-    if constexpr (PER_TOKEN) return *reinterpret_cast<const v4f*>(s + pos);
-    const float v = s[pos >> shift];
-    return v4f{v, v, v, v};
+__device__ __forceinline__ Scales load_scales(const amusd_q8_cache& C, size_t kvh, int c0) {
+    Scales s;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int pos = c0 + i * 256 + (threadIdx.x & 63) * 4;
+        s.k[i] = s.v[i] = v4f{0.f, 0.f, 0.f, 0.f};
+        if (pos < C.cap && pos < c0 + C.chunk) {
+            const size_t at = kvh * (C.cap / C.block);
+            if constexpr (PER_TOKEN) {
+                s.k[i] = *reinterpret_cast<const v4f*>(C.ks + at + pos);
+                s.v[i] = *reinterpret_cast<const v4f*>(C.vs + at + pos);
+            } else {
+                const int b = pos >> __builtin_ctz(C.block);
+                const float k = C.ks[at + b], v = C.vs[at + b];
+                s.k[i] = v4f{k, k, k, k};
+                s.v[i] = v4f{v, v, v, v};
+            }
+        }
+    }
+    return s;
 }
 
-template <int HD, bool PER_TOKEN, int NT>
-__device__ __forceinline__ void chunk_sums(const amusd_q8_cache& C, size_t kvh, const Tile<HD> (&T)[NT], int c0, int c1, Sums<HD> (&S)[NT]) {
-    const int lane = threadIdx.x & 63, g = lane >> 4;
-    const int8_t* K = C.k + kvh * ((size_t)C.cap * HD) + (size_t)(lane & 15) * HD + g * 16;
-    const uint4* V = reinterpret_cast<const uint4*>(C.v + kvh * ((size_t)C.cap * HD)) + lane;
-    const float *ks = C.ks + kvh * (C.cap / C.block), *vs = C.vs + kvh * (C.cap / C.block);
-    const int shift = __builtin_ctz(C.block);
-    // The power of two that brings each pair's weights below 2^15 (of the values that it sees in this chunk).
-    float up[NT], down[NT];
-    {
-        float most[NT] = {};
-        for (int pos = c0 + g * 4; pos < c1; pos += 16) {
-            const v4f s = key_scales<PER_TOKEN>(vs, pos, shift);
+// A step takes 64 keys: two blocks of 32, the values' unit.  (A wave issues an instruction every 4 to 12 clocks, dependent ones
+// the more slowly: one block a step took 0.82 us for a wave alone on its SIMD, two take 1.06.)
+constexpr int kStep = 64;
+template <int HD>
+struct Keys {
+    uint4 k[4][HD / 64];
+};
+template <int HD>
+struct Values {
+    uint4 v[2][HD / 32];
+};
+template <int HD>
+__device__ __forceinline__ Keys<HD> load_keys(const amusd_q8_cache& C, size_t kvh, int b) {
+    const uint4* K = reinterpret_cast<const uint4*>(C.k + kvh * ((size_t)C.cap * HD)) + (size_t)(b >> 4) * (HD / 64) * 64 + (threadIdx.x & 63);
+    Keys<HD> B;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) most[n] = fmaxf(most[n], pos + e <= T[n].pos ? s[e] : 0.f);
+        for (int f = 0; f < HD / 64; ++f) B.k[t][f] = K[(t * (HD / 64) + f) * 64];
+    return B;
+}
+template <int HD>
+__device__ __forceinline__ Values<HD> load_values(const amusd_q8_cache& C, size_t kvh, int b) {
+    const uint4* V = reinterpret_cast<const uint4*>(C.v + kvh * ((size_t)C.cap * HD)) + (size_t)(b >> 5) * (HD / 32) * 64 + (threadIdx.x & 63);
+    Values<HD> B;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d) B.v[h][d] = V[(h * (HD / 32) + d) * 64];
+    return B;
+}
+
+constexpr float kSlack = 4.f;                    // a maximum may exceed its reference by 2^4 before the sums are rescaled
+
+// A step's scores, without the query's factor.
+template <int HD>
+__device__ __forceinline__ void step_scores(const Keys<HD>& K, const Tile<HD>& T, const v4f* ks, float (&sc)[4][4]) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        v4i hi = {}, lo = {};
+#pragma unroll
+        for (int f = 0; f < HD / 64; ++f) {
+            hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, K.k[t][f]), __builtin_bit_cast(v4i, T.hi[f]), hi, 0, 0, 0);
+            lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, K.k[t][f]), __builtin_bit_cast(v4i, T.lo[f]), lo, 0, 0, 0);
         }
+        const v4f scale = ks[t * 4];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            most[n] = fmaxf(most[n], lane_xor<16>(most[n]));
-            most[n] = fmaxf(most[n], lane_xor<32>(most[n]));
-            const int e = min(max((int)(__float_as_uint(most[n]) >> 23) - 127, -110), 126);
-            up[n] = __uint_as_float((uint32_t)(127 + 14 - e) << 23);       // most * up in [2^14, 2^15)
-            down[n] = __uint_as_float((uint32_t)(127 - 14 + e) << 23);
-        }
+        for (int e = 0; e < 4; ++e) sc[t][e] = (float)(hi[e] * 256 + lo[e]) * scale[e];
     }
+}
+
+// .. and its weights, as the values' product takes them, 2^lift times what they are.  MASK: some pair does not see all of its keys.
+// left: keys from the step's first one up to the last that the lane's pair sees.
+template <int HD, bool MASK>
+__device__ __forceinline__ void step_weights(float (&sc)[4][4], float qs, const v4f* vs, float lift, int left, Sums<HD>& S, uint4 (&out)[2]) {
+    const int g4 = (threadIdx.x & 48) >> 2;
+    float top[4];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        S[n].ref = -INFINITY;
-        S[n].den = 0.f;
+    for (int t = 0; t < 4; ++t) {
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d) S[n].acc[d] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int e = 0; e < 4; ++e)
+            if (MASK && t * 16 + g4 + e > left) sc[t][e] = -INFINITY;
+        top[t] = fmaxf(fmaxf(sc[t][0], sc[t][1]), fmaxf(sc[t][2], sc[t][3]));
     }
-    for (int b = c0; b < c1; b += 32) {
-        uint4 kf[2][HD / 64], vf[HD / 32];
+    float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    most = fmaxf(most, lane_xor<16>(most));
+    most = fmaxf(most, lane_xor<32>(most)) * qs;
+    const bool grow = most > S.ref + kSlack;
+    if (__any(grow)) {
+        const float ref = grow ? most : S.ref, shrink = pow2(S.ref - (ref == -INFINITY ? 0.f : ref));    // (1 where nothing grows, or 0 * 0)
+        S.ref = ref;
+        S.den *= shrink;
+        S.weights *= shrink;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int f = 0; f < HD / 64; ++f) kf[t][f] = *reinterpret_cast<const uint4*>(K + (size_t)(b + t * 16) * HD + f * 64);
-#pragma unroll
-        for (int d = 0; d < HD / 32; ++d) vf[d] = V[((size_t)(b >> 5) * (HD / 32) + d) * 64];
-        v4f kscale[2], vscale[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            kscale[t] = key_scales<PER_TOKEN>(ks, b + t * 16 + g * 4, shift);
-            vscale[t] = key_scales<PER_TOKEN>(vs, b + t * 16 + g * 4, shift);
-        }
-        uint4 w[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float sc[2][4], top = -INFINITY;
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                v4i hi = {}, lo = {};
-#pragma unroll
-                for (int f = 0; f < HD / 64; ++f) {
-                    hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, kf[t][f]), __builtin_bit_cast(v4i, T[n].hi[f]), hi, 0, 0, 0);
-                    lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, kf[t][f]), __builtin_bit_cast(v4i, T[n].lo[f]), lo, 0, 0, 0);
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float s = (float)(hi[e] * 256 + lo[e]) * (T[n].qs * kscale[t][e]);
-                    sc[t][e] = b + t * 16 + g * 4 + e <= T[n].pos ? s : -INFINITY;
-                    top = fmaxf(top, sc[t][e]);
-                }
-            }
-            top = fmaxf(top, lane_xor<16>(top));
-            top = fmaxf(top, lane_xor<32>(top));
-            const float ref = fmaxf(S[n].ref, top), at = ref == -INFINITY ? 0.f : ref;
-            const float shrink = pow2(S[n].ref - at);
-            float sum = 0.f, p[2][4];
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[t][e] = pow2(sc[t][e] - at);
-                    sum += p[t][e];
-                    // (a key that is not seen has weight 0 whatever its value's scale is)
-                    p[t][e] *= b + t * 16 + g * 4 + e <= T[n].pos ? vscale[t][e] * up[n] : 0.f;
-                }
-            S[n].den = fmaf(S[n].den, shrink, sum);
-            S[n].ref = ref;
-#pragma unroll
-            for (int d = 0; d < HD / 16; ++d) S[n].acc[d] *= shrink;
-            auto two = [](float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, h2)); };
-            w[n] = uint4{two(p[0][0], p[0][1]), two(p[0][2], p[0][3]), two(p[1][0], p[1][1]), two(p[1][2], p[1][3])};
-        }
-#pragma unroll
-        for (int d = 0; d < HD / 32; ++d) {
-            uint4 a, c;
-            bytes_to_half(vf[d].x, a.x, a.y);
-            bytes_to_half(vf[d].y, a.z, a.w);
-            bytes_to_half(vf[d].z, c.x, c.y);
-            bytes_to_half(vf[d].w, c.z, c.w);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                S[n].acc[2 * d] = BF16::mfma_att(a, w[n], S[n].acc[2 * d]);
-                S[n].acc[2 * d + 1] = BF16::mfma_att(c, w[n], S[n].acc[2 * d + 1]);
-            }
-        }
+        for (int d = 0; d < HD / 16; ++d) S.acc[d] *= shrink;
     }
+    const float at = S.ref == -INFINITY ? 0.f : S.ref - lift;
+    float sum[4];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        S[n].den += lane_xor<16>(S[n].den);
-        S[n].den += lane_xor<32>(S[n].den);
+    for (int t = 0; t < 4; ++t) {
+        const v4f scale = vs[t * 4];
+        float p[4], w[4];
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d) S[n].acc[d] *= down[n];
+        for (int e = 0; e < 4; ++e) {
+            p[e] = pow2(fmaf(sc[t][e], qs, -at));
+            w[e] = p[e] * scale[e];
+            if (MASK && t * 16 + g4 + e > left) w[e] = 0.f;          // (whatever its value's scale is)
+        }
+        sum[t] = (p[0] + p[1]) + (p[2] + p[3]);
+        auto two = [](float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, h2)); };
+        (t & 1 ? out[t >> 1].z : out[t >> 1].x) = two(w[0], w[1]);
+        (t & 1 ? out[t >> 1].w : out[t >> 1].y) = two(w[2], w[3]);
     }
+    S.den += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
 // sums so far and a chunk's: how both are weighed
@@ -256,140 +259,285 @@ __device__ __forceinline__ void merge_weights(float& ref, float& den, float cref
     ref = to;
 }
 
+// Walks the keys [begin, end) (multiples of a step; begin a chunk's) and calls done(chunk's first key, its sums) at the end of each chunk.
+// The next step's keys are fetched as soon as a step's scores are found, its values behind the values' product: into the registers that
+// those leave free.  least: the last key that all pairs see.
+template <int HD, bool PER_TOKEN, class Done>
+__device__ __forceinline__ void walk(const amusd_q8_cache& C, size_t kvh, const Tile<HD>& T, int least, int begin, int end, Keys<HD> K, Scales sc,
+                                     float* lds, Done&& done) {
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    v4f* const kl = reinterpret_cast<v4f*>(lds);
+    v4f* const vl = reinterpret_cast<v4f*>(lds + kMaxChunk);
+    Sums<HD> S;
+    float lift = 0.f;
+    int c0 = begin;
+    auto chunk_begin = [&](int b) {
+        c0 = b;
+        __builtin_amdgcn_wave_barrier();
+        float all = 0.f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            kl[i * 64 + lane] = sc.k[i];
+            vl[i * 64 + lane] = sc.v[i];
+            all = fmaxf(all, fmaxf(fmaxf(sc.v[i][0], sc.v[i][1]), fmaxf(sc.v[i][2], sc.v[i][3])));
+        }
+        __builtin_amdgcn_wave_barrier();
+        // The power of two that brings each pair's weights below 2^15: the largest scale among the values that it sees here to [2^10, 2^11).
+        float most = 0.f;
+        if (least >= c0 + C.chunk - 1) {                    // (the same in all lanes)
+            most = fmaxf(all, lane_xor<1>(all));
+            most = fmaxf(most, lane_xor<2>(most));
+            most = fmaxf(most, lane_xor<4>(most));
+            most = fmaxf(most, lane_xor<8>(most));
+        } else {
+            for (int k = g * 4; k < min(C.chunk, end - c0); k += 16) {
+                const v4f s = vl[k >> 2];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = fmaxf(most, c0 + k + e <= T.pos ? s[e] : 0.f);
+            }
+        }
+        most = fmaxf(most, lane_xor<16>(most));
+        most = fmaxf(most, lane_xor<32>(most));
+        lift = (float)(10 - min(max((int)(__float_as_uint(most) >> 23) - 127, -100), 100));
+        S.ref = -INFINITY;
+        S.den = 0.f;
+        S.weights = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d) S.acc[d] = v4f{0.f, 0.f, 0.f, 0.f};
+    };
+    Values<HD> V = load_values<HD>(C, kvh, begin);
+    for (int b = begin; b < end; b += kStep) {
+        if (!(b & (C.chunk - 1))) chunk_begin(b);
+        const bool more = b + kStep < end, ends = !((b + kStep) & (C.chunk - 1)) || !more;
+        const v4f* const ks = kl + ((b - c0) >> 2) + g;
+        const v4f* const vs = vl + ((b - c0) >> 2) + g;
+        float sc4[4][4];
+        step_scores<HD>(K, T, ks, sc4);
+        if (more) K = load_keys<HD>(C, kvh, b + kStep);
+        if (ends && more) sc = load_scales<PER_TOKEN>(C, kvh, b + kStep);
+        uint4 w[2];
+        if (b + kStep - 1 <= least) step_weights<HD, false>(sc4, T.qs, vs, lift, 0, S, w);
+        else step_weights<HD, true>(sc4, T.qs, vs, lift, T.pos - b, S, w);
+        const uint4 ones{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            S.weights = BF16::mfma_att(ones, w[h], S.weights);
+#pragma unroll
+            for (int d = 0; d < HD / 32; ++d) {
+                uint4 a, c;
+                bytes_to_half(V.v[h][d].x, a.x, a.y);
+                bytes_to_half(V.v[h][d].y, a.z, a.w);
+                bytes_to_half(V.v[h][d].z, c.x, c.y);
+                bytes_to_half(V.v[h][d].w, c.z, c.w);
+                S.acc[2 * d] = BF16::mfma_att(a, w[h], S.acc[2 * d]);
+                S.acc[2 * d + 1] = BF16::mfma_att(c, w[h], S.acc[2 * d + 1]);
+                __builtin_amdgcn_sched_barrier(0);           // (all values converted first would take 64 registers)
+            }
+        }
+        if (more) V = load_values<HD>(C, kvh, b + kStep);
+        if (ends) {
+            const float down = __uint_as_float((uint32_t)(127 - (int)lift) << 23);
+            S.den += lane_xor<16>(S.den);
+            S.den += lane_xor<32>(S.den);
+            S.den *= down;
+#pragma unroll
+            for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) S.acc[d][e] = fmaf(-1152.f, S.weights[e], S.acc[d][e]) * down;
+            done(c0, S);
+        }
+    }
+}
+
 __device__ __forceinline__ int find_seg(const Q8Segs& S, int unit) {
     int i = 0;
     while (i + 1 < S.n_seg && unit >= S.s[i + 1].unit0) ++i;
     return i;
 }
 
-// A wave: one tile, one chunk.  Its sums go to memory.
-template <int HD, bool PER_TOKEN>
-__global__ void __launch_bounds__(64) k_q8_att_part(amusd_q8_cache C, int layer, Q8Segs S, Q8Query Q) {
-    const int chunk = blockIdx.x, tile = blockIdx.y, kvh = blockIdx.z;
-    const Q8Seg& seg = S.s[find_seg(S, tile)];
-    const int local = tile - seg.unit0;
-    const int last = seg.pos0 + min((local * 16 + 15) / C.G, seg.n - 1);        // the last key that a pair of the tile sees
-    const int c0 = chunk * C.chunk;
-    if (c0 > last) return;
-    Tile<HD> T[1] = {load_tile<HD>(C, Q, seg, kvh, local)};
-    Sums<HD> sums[1];
-    const size_t head = ((size_t)layer * C.n_seqs + seg.seq) * C.Hkv + kvh;
-    chunk_sums<HD, PER_TOKEN, 1>(C, head, T, c0, min(c0 + C.chunk, (last + 32) / 32 * 32), sums);
-    const int lane = threadIdx.x, g = lane >> 4, pair = lane & 15;
-    float* out = C.part + (((size_t)tile * C.Hkv + kvh) * C.max_chunks + chunk) * ((HD + 2) * 16);
-#pragma unroll
-    for (int d = 0; d < HD / 16; ++d)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) out[(d * 16 + g * 4 + e) * 16 + pair] = sums[0].acc[d][e];
-    if (g == 0) {
-        out[HD * 16 + pair] = sums[0].ref;
-        out[(HD + 1) * 16 + pair] = sums[0].den;
-    }
+// What a wave works on: tile `tile` of all sequences' tiles.
+struct Work {
+    const Q8Seg* seg;
+    int local, least, last;                     // the sequence's tile; the last key that its first pair sees, and that any does
+    size_t head;
+};
+__device__ __forceinline__ Work find_work(const amusd_q8_cache& C, const Q8Segs& S, int layer, int tile, int kvh) {
+    Work w;
+    w.seg = &S.s[find_seg(S, tile)];
+    w.local = tile - w.seg->unit0;
+    w.least = w.seg->pos0 + w.local * 16 / C.G;
+    w.last = w.seg->pos0 + min((w.local * 16 + 15) / C.G, w.seg->n - 1);
+    w.head = ((size_t)layer * C.n_seqs + w.seg->seq) * C.Hkv + kvh;
+    return w;
 }
 
-__device__ __forceinline__ uint16_t q8_bf16(float v) { return (uint16_t)(v == v ? bf16_rne(v) : 0x7FC0u); }
+// A wave: a tile, one chunk.  Its sums go to memory.
+template <int HD, bool PER_TOKEN>
+__global__ void __launch_bounds__(64, HD == 64 ? 3 : 1) k_q8_att_part(amusd_q8_cache C, int layer, Q8Segs S, Q8Query Q) {
+    __shared__ float lds[2 * kMaxChunk];
+    const int kvh = blockIdx.x, tile = blockIdx.y, chunk = blockIdx.z, c0 = chunk * C.chunk;       // a kv head's waves on one XCD
+    const Work W = find_work(C, S, layer, tile, kvh);
+    if (c0 > W.last) return;
+    const size_t head = W.head;
+    const Keys<HD> keys = load_keys<HD>(C, head, c0);
+    const Scales sc = load_scales<PER_TOKEN>(C, head, c0);
+    const Tile<HD> T = load_tile<HD>(C, Q, *W.seg, kvh, W.local);
+    const int lane = threadIdx.x, g = lane >> 4, pair = lane & 15;
+    walk<HD, PER_TOKEN>(C, head, T, W.least, c0, min(c0 + C.chunk, (W.last + kStep) / kStep * kStep), keys, sc, lds, [&](int, const Sums<HD>& sums) {
+        float* out = C.part + (((size_t)tile * C.Hkv + kvh) * C.max_chunks + chunk) * ((HD + 2) * 16);
+#pragma unroll
+        for (int d = 0; d < HD / 16; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[(d * 16 + g * 4 + e) * 16 + pair] = sums.acc[d][e];
+        if (g == 0) {
+            out[HD * 16 + pair] = sums.ref;
+            out[(HD + 1) * 16 + pair] = sums.den;
+        }
+    });
+}
 
-// A workgroup merges a tile's chunks: thread (column, pair).
+__device__ __forceinline__ uint16_t q8_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+
+// A workgroup merges HD / 8 columns of a tile: thread (column, pair).  How each chunk is weighed follows from the references alone: found
+// for up to 64 chunks at a time by as many threads, while the sums are on their way; those are then added up in order.
 template <int HD>
-__global__ void __launch_bounds__(HD * 4) k_q8_att_merge(amusd_q8_cache C, Q8Segs S, Q8Query Q) {
-    const int tile = blockIdx.x, kvh = blockIdx.y, part = blockIdx.z;           // a quarter of the columns a workgroup
+__global__ void __launch_bounds__(HD * 2) k_q8_att_merge(amusd_q8_cache C, Q8Segs S, Q8Query Q) {
+    constexpr int kAtOnce = 16, kRound = 64, kPart = (HD + 2) * 16, kThreadsOf = HD * 2;
+    __shared__ float refs[kRound][16], dens[kRound][16], upto[kRound + 1][16];
+    __shared__ v4f how[kRound][16];                          // what is done with a chunk: the sums before it times [0], its own times [1]; [2] its denominator
+    const int kvh = blockIdx.x, tile = blockIdx.y, t = threadIdx.x;
     const Q8Seg& seg = S.s[find_seg(S, tile)];
-    const int pair = threadIdx.x & 15, col = part * (HD / 4) + (threadIdx.x >> 4);
-    const int p = (tile - seg.unit0) * 16 + pair;
-    if (p >= seg.n * C.G) return;
-    const int row = p / C.G, head = kvh * C.G + p % C.G;
-    const int chunks = (seg.pos0 + row) / C.chunk + 1;
-    const float* in = C.part + ((size_t)tile * C.Hkv + kvh) * C.max_chunks * ((HD + 2) * 16) + pair;
-    float ref = -INFINITY, den = 0.f, acc = 0.f;
-    for (int c = 0; c < chunks; ++c, in += (HD + 2) * 16) {
-        float a, b;
-        merge_weights(ref, den, in[HD * 16], in[(HD + 1) * 16], a, b);
-        acc = fmaf(acc, a, in[col * 16] * b);
+    const int first = (tile - seg.unit0) * 16, pairs = min(16, seg.n * C.G - first);
+    const int pair = t & 15, col = blockIdx.z * (HD / 8) + (t >> 4);
+    auto chunks_of = [&](int p) { return (seg.pos0 + (first + p) / C.G) / C.chunk + 1; };
+    const int mine = chunks_of(min(pair, pairs - 1)), most = chunks_of(pairs - 1);
+    const float* const part = C.part + ((size_t)tile * C.Hkv + kvh) * C.max_chunks * kPart;
+    float ref = -INFINITY, den = 0.f, acc = 0.f;             // ref: the largest of the rounds before (threads 0 to 15)
+    for (int c0 = 0; c0 < most; c0 += kRound) {
+        const int n = min(kRound, most - c0);
+        float x[kAtOnce];
+        auto fetch = [&](int from) {
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) x[i] = part[(size_t)min(from + i, most - 1) * kPart + col * 16 + pair];
+        };
+        for (int i = t; i < n * 32; i += kThreadsOf) {       // (references and denominators lie together)
+            const float v = part[(size_t)(c0 + (i >> 5)) * kPart + HD * 16 + (i & 31)];
+            (i & 16 ? dens : refs)[i >> 5][pair] = v;
+        }
+        fetch(c0);
+        __syncthreads();
+        if (t < 16) {
+            upto[0][t] = ref;
+            for (int c = 0; c < n; c += 16) {
+                float r[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) r[i] = refs[min(c + i, n - 1)][t];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    ref = fmaxf(ref, r[i]);
+                    if (c + i < n) upto[c + i + 1][t] = ref;
+                }
+            }
+        }
+        __syncthreads();
+        for (int i = t; i < n * 16; i += kThreadsOf) {
+            const int c = i >> 4;
+            const float to = upto[c + 1][pair], at = to == -INFINITY ? 0.f : to;
+            const float b = pow2(refs[c][pair] - at);
+            how[c][pair] = v4f{pow2(upto[c][pair] - at), b, dens[c][pair] * b, 0.f};
+        }
+        __syncthreads();
+        for (int c = 0; c < n; c += kAtOnce) {
+            if (c) fetch(c0 + c);
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                const v4f h = how[min(c + i, n - 1)][pair];
+                const float d = fmaf(den, h[0], h[2]), s = fmaf(acc, h[0], x[i] * h[1]);
+                const bool sees = c0 + c + i < mine && c + i < n;       // (a chunk that the pair sees nothing of is not merged)
+                den = sees ? d : den;
+                acc = sees ? s : acc;
+            }
+        }
+        if (c0 + kRound < most) __syncthreads();
     }
+    if (pair >= pairs) return;
+    const int row = (first + pair) / C.G, head = kvh * C.G + (first + pair) % C.G;
     Q.out[(int64_t)(seg.row0 + row) * Q.ldo + (int64_t)head * HD + col] = q8_bf16(acc / den);
 }
 
-// A wave: NT neighbouring tiles, all chunks, merged in registers.
-template <int HD, bool PER_TOKEN, int NT>
-__global__ void __launch_bounds__(64) k_q8_att_whole(amusd_q8_cache C, int layer, Q8Segs S, Q8Query Q) {
-    const int unit = gridDim.x - 1 - blockIdx.x, kvh = blockIdx.y;              // the longest first
-    const Q8Seg& seg = S.s[find_seg(S, unit)];
-    const int local = (unit - seg.unit0) * NT, tiles = (seg.n * C.G + 15) / 16;
-    Tile<HD> T[NT];
-    Sums<HD> all[NT];
+// A wave: a tile, all chunks.  The sums over the chunks so far wait in LDS, where they are touched once a chunk.
+template <int HD, bool PER_TOKEN>
+__global__ void __launch_bounds__(64, HD == 64 ? 3 : 2) k_q8_att_whole(amusd_q8_cache C, int layer, Q8Segs S, Q8Query Q) {
+    __shared__ float lds[2 * kMaxChunk];
+    __shared__ v4f all[HD / 16][64];
+    const int kvh = blockIdx.x, lane = threadIdx.x;                             // a kv head's waves on one XCD, the longest first
+    const Work W = find_work(C, S, layer, gridDim.y - 1 - blockIdx.y, kvh);
+    const Tile<HD> T = load_tile<HD>(C, Q, *W.seg, kvh, W.local);
+    __builtin_amdgcn_sched_barrier(0);
+    const Keys<HD> keys = load_keys<HD>(C, W.head, 0);
+    const Scales sc = load_scales<PER_TOKEN>(C, W.head, 0);
+    float ref = -INFINITY, den = 0.f;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        T[n] = load_tile<HD>(C, Q, seg, kvh, min(local + n, tiles - 1));
-        if (local + n >= tiles) T[n].pos = -1;
-        all[n].ref = -INFINITY;
-        all[n].den = 0.f;
-#pragma unroll
-        for (int d = 0; d < HD / 16; ++d) all[n].acc[d] = v4f{0.f, 0.f, 0.f, 0.f};
-    }
-    const int last = seg.pos0 + min((local * 16 + NT * 16 - 1) / C.G, seg.n - 1);
-    const size_t head = ((size_t)layer * C.n_seqs + seg.seq) * C.Hkv + kvh;
-    for (int c0 = 0; c0 <= last; c0 += C.chunk) {
-        Sums<HD> part[NT];
-        chunk_sums<HD, PER_TOKEN, NT>(C, head, T, c0, min(c0 + C.chunk, (last + 32) / 32 * 32), part);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if (c0 > T[n].pos) continue;                    // a chunk that the pair sees nothing of is not merged
-            float a, b;
-            merge_weights(all[n].ref, all[n].den, part[n].ref, part[n].den, a, b);
-#pragma unroll
-            for (int d = 0; d < HD / 16; ++d)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) all[n].acc[d][e] = fmaf(all[n].acc[d][e], a, part[n].acc[d][e] * b);
-        }
-    }
-    const int g = (threadIdx.x & 63) >> 4;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        if (T[n].pos < 0) continue;
-        uint16_t* out = Q.out + (int64_t)(seg.row0 + T[n].row) * Q.ldo + (int64_t)T[n].head * HD + g * 4;
+    for (int d = 0; d < HD / 16; ++d) all[d][lane] = v4f{0.f, 0.f, 0.f, 0.f};
+    walk<HD, PER_TOKEN>(C, W.head, T, W.least, 0, (W.last + kStep) / kStep * kStep, keys, sc, lds, [&](int c0, const Sums<HD>& part) {
+        if (c0 > T.pos) return;                             // a chunk that the pair sees nothing of is not merged
+        float a, b;
+        merge_weights(ref, den, part.ref, part.den, a, b);
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d) {
-            uint16_t b[4];
+            v4f v = all[d][lane];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) b[e] = q8_bf16(all[n].acc[d][e] / all[n].den);
-            __builtin_memcpy(out + d * 16, b, 8);
+            for (int e = 0; e < 4; ++e) v[e] = fmaf(v[e], a, part.acc[d][e] * b);
+            all[d][lane] = v;
         }
+    });
+    if (T.pos < 0) return;
+    const int pair = W.local * 16 + (lane & 15);
+    uint16_t* out = Q.out + (int64_t)(W.seg->row0 + pair / C.G) * Q.ldo + (int64_t)(kvh * C.G + pair % C.G) * HD + (lane >> 4) * 4;
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d) {
+        uint16_t b[4];
+        const v4f v = all[d][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] = q8_bf16(v[e] / den);
+        __builtin_memcpy(out + d * 16, b, 8);
     }
 }
 
 void q8_attention_plan(amusd_q8_cache& c) {
-    // A chunk is a wave's work where there are few rows: with a full cache there should be a few waves a compute unit.
-    int chunk = 64;
-    while (chunk < 256 && (int64_t)c.cap / chunk * c.Hkv > 2 * c.cus) chunk *= 2;
+    // A chunk is a wave's work where there are few rows.  Short, for a wave on every other compute unit from one tile's full cache; no
+    // shorter, as a chunk costs a wave its beginning and end (64 keys of 64 a step: 450 instructions a step, of 512: 300) and has
+    // sums to write and to merge.  us, chunks of 64 / 128 / 256 / 512: 1B shape, 1 row, 512 keys 8.6 / 8.9 / 10.3 / 13.3, 4000 keys - /
+    // 11.0 / 10.8 / 14.1; 8B shape, 8 rows, 2048 keys 12.9 / 12.8 / 13.0 / 16.6; 2048 rows 102 / 88 / 82 / 78.
+    int chunk = kStep;
+    while (chunk < kMaxChunk && (int64_t)c.cap / chunk * c.Hkv > c.cus / 2) chunk *= 2;
     c.chunk = chunk;
     c.max_chunks = (c.cap + chunk - 1) / chunk;
-    c.part_tiles = (kMaxSegs * c.G + 15) / 16 + kMaxSegs;       // 16 rows in up to 16 sequences, and each sequence's last tile
-    c.part_tiles *= c.Hkv;
+    // Tiles whose chunks are split over waves: while there are fewer than five for four compute units (8B shape, 100 rows behind 1000 keys, 200
+    // tiles: 21 us against 29 for a wave a tile; 250 rows, 504 tiles: 43 against 34).  64 MB of sums at most, but those of 16 rows always.
+    const int64_t tile_bytes = (int64_t)c.max_chunks * (c.hd + 2) * 16 * 4;
+    const int64_t least = (kMaxSegs + (kMaxSegs * c.G + 15) / 16) * (int64_t)c.Hkv;
+    c.part_tiles = (int)std::max(least, std::min<int64_t>(c.cus * 5 / 4, (64 << 20) / tile_bytes));
 }
 
 hipError_t launch_q8_attention(const amusd_q8_cache& c, int layer, const Q8Segs& segs, const void* q, int64_t ldq, float scale, const float* cos,
                                const float* sin, void* out, int64_t ldo, hipStream_t stream) {
     Q8Segs S = segs;
     const Q8Query Q{static_cast<const uint16_t*>(q), ldq, static_cast<uint16_t*>(out), ldo, cos, sin, scale * 1.44269504088896340736f};
-    auto units = [&](int per) {
-        int n = 0;
-        for (int i = 0; i < S.n_seg; ++i) {
-            S.s[i].unit0 = n;
-            n += ((S.s[i].n * c.G + 15) / 16 + per - 1) / per;
-        }
-        return n;
-    };
+    int64_t tiles = 0;
+    for (int i = 0; i < S.n_seg; ++i) {
+        S.s[i].unit0 = (int)tiles;
+        tiles += ((int64_t)S.s[i].n * c.G + 15) / 16;
+    }
     auto go = [&](auto hd, auto per_token) {
         constexpr int HD = decltype(hd)::value;
         constexpr bool PT = decltype(per_token)::value;
-        const int tiles = units(1);
         if (tiles * c.Hkv <= c.part_tiles) {
             const int chunks = (S.max_len + c.chunk - 1) / c.chunk;
-            hipLaunchKernelGGL((k_q8_att_part<HD, PT>), dim3(chunks, tiles, c.Hkv), dim3(64), 0, stream, c, layer, S, Q);
-            hipLaunchKernelGGL((k_q8_att_merge<HD>), dim3(tiles, c.Hkv, 4), dim3(HD * 4), 0, stream, c, S, Q);
+            hipLaunchKernelGGL((k_q8_att_part<HD, PT>), dim3(c.Hkv, (unsigned)tiles, chunks), dim3(64), 0, stream, c, layer, S, Q);
+            hipLaunchKernelGGL((k_q8_att_merge<HD>), dim3(c.Hkv, (unsigned)tiles, 8), dim3(HD * 2), 0, stream, c, S, Q);
         } else {
-            const int u = units(2);
-            hipLaunchKernelGGL((k_q8_att_whole<HD, PT, 2>), dim3(u, c.Hkv), dim3(64), 0, stream, c, layer, S, Q);
+            hipLaunchKernelGGL((k_q8_att_whole<HD, PT>), dim3(c.Hkv, (unsigned)tiles), dim3(64), 0, stream, c, layer, S, Q);
         }
     };
     auto by_block = [&](auto hd) {

@@ -281,8 +281,8 @@ int amusd_generate_greedy(amusd_model *m, const int32_t *prompt, int32_t n_promp
  * the parts of a decoder layer that holds both in 8 bits: rows to 8 bits, with or without an RMS norm in front, the
  * product of such rows with an 8-bit matrix, and attention over a cache in 8 bits.
  *
- * 8 bits stand for x ~ q * s, q an integer in [-127, 127]: s = max|x| / 127 over the values that share the scale, q = x / s
- * rounded to the nearest integer, ties to even.  s = 0 where all values are 0.  Values that are not finite give
+ * 8 bits stand for x ~ q * s, q an integer in [-127, 127]: s = max|x| / 127 over the values that share the scale, q the quotient
+ * x / s (both in float32) rounded to the nearest integer, ties to even.  s = 0 where all values are 0.  Values that are not finite give
  * s = NaN and q = 0, so that what is computed from them is NaN too.
  *
  * All pointers are device memory of the current device unless said otherwise, but arrays of sequence ids, positions and
@@ -298,8 +298,8 @@ int amusd_q8_quantize(const void *x, int32_t dtype, int64_t ldx, int32_t rows, i
                       float *scale, void *hip_stream);
 
 /* The RMS norm in front of a projection: s = x + add (add may be NULL; fp32 or bf16, add_dtype), sum = s in x's type (sum may
- * be NULL, or x itself), y = s / sqrt(mean(s^2) + eps) * gain, and y in 8 bits as amusd_q8_quantize has it.  Squares and
- * norms are taken in 64 bits, from s before it is rounded to sum.  gain: fp32 [n].  sum = x in bf16: n at most 16384. */
+ * be NULL, or x itself), y = s / sqrt(mean(s^2) + eps) * gain, taken in 64 bits from s before that is rounded to
+ * sum and rounded to float32, and y in 8 bits as amusd_q8_quantize has it.  gain: fp32 [n].  sum = x in bf16: n at most 16384. */
 int amusd_q8_rmsnorm(const void *x, int32_t dtype, int64_t ldx, const void *add, int32_t add_dtype, int64_t ldadd,
                      const float *gain, float eps, int32_t rows, int32_t n, void *sum, int64_t ldsum, int8_t *q,
                      int64_t ldq, float *scale, void *hip_stream);

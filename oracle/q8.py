@@ -11,13 +11,15 @@ def bf16(x):
 
 
 def quantize(x):
-    """Rows in 8 bits: integers, float32 scales, and the distance of every quotient from the nearest border between integers."""
-    x = np.asarray(x, dtype=np.float64)
+    """Rows, rounded to float32, in 8 bits: integers, float32 scales, and the distance of every float32 quotient from the nearest border
+    between integers."""
+    x = np.asarray(x, dtype=np.float64).astype(np.float32)
     bad = ~np.isfinite(x).all(-1)
     most = np.abs(np.where(np.isfinite(x), x, 0)).max(-1)
-    scale = np.where(bad, np.nan, most / 127).astype(np.float32)
+    scale = np.where(bad, np.float32(np.nan), most / np.float32(127))
     live = (scale > 0) & ~bad
-    t = np.where(live[..., None], x / np.where(live, scale, 1).astype(np.float64)[..., None], 0)
+    with np.errstate(invalid="ignore"):
+        t = np.where(live[..., None], x / np.where(live, scale, np.float32(1))[..., None], 0).astype(np.float64)
     t = np.where(np.isfinite(t), t, 0)
     return np.clip(np.rint(t), -127, 127).astype(np.int64), scale, np.abs(np.abs(t - np.floor(t)) - 0.5)
 

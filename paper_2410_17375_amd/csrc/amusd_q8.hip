@@ -14,11 +14,12 @@ namespace amusd {
 
 // ---------------------------------------------------------------- rows to 8 bits
 // A workgroup a row, the row in registers: it is read once and written once, so the bytes bound it (and its launch, where
-// there are few rows).  Squares are summed and rows divided in 64 bits: a square of a large element stays finite, and an
-// element is rounded to the wrong one of two neighbours only if it is nearer than 2^-50 to their middle.
-// Loads and stores take any alignment (one instruction of 16 bytes all the same).
+// there are few rows).  Loads and stores take any alignment (one instruction of 16 bytes all the same).  Sums of squares, their root and the normalised
+// element are in 64 bits, the element then rounded to 32: a square of a large element stays finite.
+// The quotient is taken as the product with the scale's reciprocal, and divided in full only where that is too near the middle between
+// two integers to tell (half the largest value stands on one); adding 1.5 * 2^23 leaves the nearest integer, ties to even, in the low bits.
 template <class T>
-__device__ __forceinline__ void q8_load(const T* p, int n, float (&v)[8]) {       // n: elements there are, 1..8
+__device__ __forceinline__ void q8_load(const T* p, int n, float (&v)[8]) {       // n: elements there are, 1 or more
     T e[8];
     if (n >= 8) {
         __builtin_memcpy(e, p, 8 * sizeof(T));
@@ -37,12 +38,8 @@ __device__ __forceinline__ void q8_store(T* p, int n, const float (&v)[8]) {
     T e[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        if constexpr (sizeof(T) == 2) {
-            const uint32_t b = bf16_rne(v[i]);
-            e[i] = (T)(v[i] == v[i] ? b : 0x7FC0u);                              // the rounding's carry could end a NaN
-        } else {
-            e[i] = __float_as_uint(v[i]);
-        }
+        if constexpr (sizeof(T) == 2) e[i] = __builtin_bit_cast(uint16_t, (__bf16)v[i]);
+        else e[i] = __float_as_uint(v[i]);
     }
     if (n >= 8) {
         __builtin_memcpy(p, e, 8 * sizeof(T));
@@ -53,154 +50,165 @@ __device__ __forceinline__ void q8_store(T* p, int n, const float (&v)[8]) {
     }
 }
 
+template <int OFF>
+__device__ __forceinline__ double lane_xor(double v) {
+    const uint64_t b = (uint64_t)__double_as_longlong(v);
+    return __longlong_as_double((long long)((uint64_t)lane_xor_u<OFF>((uint32_t)(b >> 32)) << 32 | lane_xor_u<OFF>((uint32_t)b)));
+}
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
+    v += lane_xor<1>(v);
+    v += lane_xor<2>(v);
+    v += lane_xor<4>(v);
+    v += lane_xor<8>(v);
+    v += lane_xor<16>(v);
+    return v + lane_xor<32>(v);
 }
-__device__ __forceinline__ double wave_max(double v) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v = fmax(v, __shfl_xor(v, off, 64));
-    return v;
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    v = max(v, lane_xor_u<1>(v));
+    v = max(v, lane_xor_u<2>(v));
+    v = max(v, lane_xor_u<4>(v));
+    v = max(v, lane_xor_u<8>(v));
+    v = max(v, lane_xor_u<16>(v));
+    return max(v, lane_xor_u<32>(v));
 }
-// Over a workgroup; every thread gets the result.
-template <class F>
-__device__ __forceinline__ double group_reduce(double v, double* lds, F wave_op, bool is_max) {
-    const int waves = blockDim.x >> 6;
-    v = wave_op(v);
-    if (waves == 1) return v;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    double r = lds[0];
-    for (int w = 1; w < waves; ++w) r = is_max ? fmax(r, lds[w]) : r + lds[w];
-    return r;
+
+// The scale of values whose largest magnitude has these bits (those of a NaN are above all others), and its reciprocal, 0 where there is none.
+__device__ __forceinline__ float q8_scale(uint32_t bits, float& inv) {
+    if (bits >= 0x7F800000u) {
+        inv = 0.f;
+        return __uint_as_float(0x7FC00000u);
+    }
+    const float s = (float)((double)__uint_as_float(bits) / 127.);
+    inv = s > 0.f ? (float)(1. / (double)s) : 0.f;
+    return s;
+}
+// Low bytes: the float32 quotients v[i] / s rounded to the nearest integer (0 where there is no scale).
+template <int N>
+__device__ __forceinline__ void q8_round(const float (&v)[N], float s, float inv, uint32_t (&b)[N]) {
+    float far = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float t = v[i] * inv, r = t + 12582912.f;
+        far = fmaxf(far, fabsf(t - (r - 12582912.f)));
+        b[i] = inv > 0.f ? __float_as_uint(r) : 0u;
+    }
+    if (far > 0.49998f && inv > 0.f)             // (t is off by at most 127 * 2^-23)
+#pragma unroll
+        for (int i = 0; i < N; ++i) b[i] = (uint32_t)(int)rintf(v[i] / s);
+}
+__device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
 }
 
 // X, A: bits of the input's and the addend's elements.  kHeld: vectors of 8 that a thread keeps (0: rows too long for that are read
 // again).  NORM: with an RMS norm in front.
 template <class X, class A, bool NORM, int kHeld>
-__global__ void __launch_bounds__(1024) k_q8_rows(const X* x, int64_t ldx, const A* __restrict__ add, int64_t ldadd,
-                                                  const float* __restrict__ gain, float eps, int n, X* sum, int64_t ldsum, int8_t* __restrict__ q,
-                                                  int64_t ldq, float* __restrict__ scale) {
-    __shared__ double lds[16];
+__global__ void __launch_bounds__(1024) k_q8_rows(const X* x, int64_t ldx, const A* __restrict__ add, int64_t ldadd, const float* __restrict__ gain, float eps,
+                                                  int n, X* sum, int64_t ldsum, int8_t* __restrict__ q, int64_t ldq, float* __restrict__ scale) {
+    __shared__ double sums[16];
+    __shared__ uint32_t tops[16];
     const int64_t row = blockIdx.x;
     x += row * ldx;
     q += row * ldq;
     if (add) add += row * ldadd;
     if (sum) sum += row * ldsum;
-    const int stride = blockDim.x * 8, first = threadIdx.x * 8;
-    constexpr int kKeep = kHeld ? kHeld : 1;
-    float held[kKeep][8];
-    auto fetch = [&](int i, int at, float (&v)[8], bool from_memory) {    // x + add of the thread's i-th vector
-        if (!from_memory) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = held[kHeld ? i : 0][e];
-            return;
-        }
-        q8_load(x + at, n - at, v);
-        if (NORM && add) {
-            float a[8];
-            q8_load(add + at, n - at, a);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += a[e];
-        }
-    };
-    double squares = 0.;
-    double most = 0.;
-    bool bad = false;
-    auto first_pass = [&](int i, int at) {
-        float v[8];
-        fetch(i, at, v, true);
-        if (NORM && sum) q8_store(sum + at, n - at, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (kHeld) held[kHeld ? i : 0][e] = v[e];
-            bad |= !(fabsf(v[e]) <= 3.402823466e38f);
-            if (NORM) squares += (double)v[e] * (double)v[e];
-            else most = fmax(most, (double)fabsf(v[e]));
-        }
-    };
-    if constexpr (kHeld > 0) {
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i)
-            if (first + i * stride < n) first_pass(i, first + i * stride);
-    } else {
-        for (int at = first; at < n; at += stride) first_pass(0, at);
-    }
-    // Rows longer than the registers are read again, from `sum` if it took the place of x (in full precision only where sum is fp32,
-    // so the host has no bf16 row of that length written over itself).
-    const bool over = !kHeld && NORM && sum == x;
-    double rstd = 1.;
-    if (NORM) rstd = 1. / sqrt(group_reduce(squares, lds, wave_sum, false) / n + (double)eps);
-    auto normed = [&](int i, int at, double (&y)[8]) {
-        float v[8];
-        if (over) q8_load(x + at, n - at, v);
-        else fetch(i, at, v, !kHeld);
-        float g[8];
-        if (NORM) q8_load(reinterpret_cast<const uint32_t*>(gain) + at, n - at, g);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = NORM ? (double)v[e] * rstd * (double)g[e] : (double)v[e];
-    };
-    if (NORM) {
-        auto second_pass = [&](int i, int at) {
-            double y[8];
-            normed(i, at, y);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                most = fmax(most, fabs(y[e]));
-                bad |= !(fabs(y[e]) <= 3.402823466e38);
-            }
-        };
+    const int stride = blockDim.x * 8, first = threadIdx.x * 8, waves = blockDim.x >> 6;
+    float held[kHeld ? kHeld : 1][8], gains[kHeld ? kHeld : 1][8];
+    // f(i, at, v) for each of the thread's vectors
+    auto vectors = [&](auto f) {
         if constexpr (kHeld > 0) {
 #pragma unroll
             for (int i = 0; i < kHeld; ++i)
-                if (first + i * stride < n) second_pass(i, first + i * stride);
+                if (first + i * stride < n) f(i, first + i * stride);
         } else {
-            for (int at = first; at < n; at += stride) second_pass(0, at);
+            for (int at = first; at < n; at += stride) f(0, at);
         }
-    }
-    most = group_reduce(bad ? INFINITY : most, lds, wave_max, true);
-    const bool finite = most <= 3.402823466e38;
-    const float s = finite ? (float)(most / 127.) : __uint_as_float(0x7FC00000u);
-    const double inv = finite && s > 0.f ? 1. / (double)s : 0.;
-    if (threadIdx.x == 0) scale[row] = s;
-    auto last_pass = [&](int i, int at) {
-        double y[8];
-        normed(i, at, y);
-        int8_t b[8];
+    };
+    auto fetch = [&](int i, int at, bool summed) {                   // summed: what is in x's place is the sum already
+        q8_load(x + at, n - at, held[i]);
+        if (NORM && add && !summed) {
+            float a[8];
+            q8_load(add + at, n - at, a);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            double t = y[e] * inv;
-            if (fabs(fabs(t - rint(t)) - 0.5) < 1e-9) t = y[e] / (double)s;      // (the product may be off a tie that the quotient hits)
-            b[e] = finite && s > 0.f ? (int8_t)(int)fmin(fmax(rint(t), -127.), 127.) : (int8_t)0;
+            for (int e = 0; e < 8; ++e) held[i][e] += a[e];
         }
+    };
+    // Rows longer than the registers are read again, from `sum` if it took the place of x (the host has no bf16 row of that length written
+    // over itself, as its sum would be a rounded one).
+    const bool over = NORM && sum == x;
+    double rstd = 1.;
+    if constexpr (NORM) {
+        double squares = 0.;
+        vectors([&](int i, int at) {
+            fetch(i, at, false);
+            if (kHeld) q8_load(reinterpret_cast<const uint32_t*>(gain) + at, n - at, gains[i]);
+            if (sum) q8_store(sum + at, n - at, held[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) squares = fma((double)held[i][e], (double)held[i][e], squares);
+        });
+        squares = wave_sum(squares);
+        if (waves > 1) {
+            if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = squares;
+            __syncthreads();
+            squares = sums[0];
+            for (int w = 1; w < waves; ++w) squares += sums[w];
+        }
+        rstd = 1. / sqrt(squares / n + (double)eps);
+    }
+    auto normed = [&](int i, int at) {                               // held[i] from x + add to what is rounded
+        if constexpr (NORM) {
+            if (!kHeld) q8_load(reinterpret_cast<const uint32_t*>(gain) + at, n - at, gains[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) held[i][e] = (float)((double)held[i][e] * rstd * (double)gains[i][e]);
+        }
+    };
+    uint32_t top = 0;
+    vectors([&](int i, int at) {
+        if (!NORM || !kHeld) fetch(i, at, over);
+        normed(i, at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(held[i][e]) & 0x7FFFFFFFu);
+    });
+    top = wave_max(top);
+    if (waves > 1) {
+        if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+        __syncthreads();
+        top = tops[0];
+        for (int w = 1; w < waves; ++w) top = max(top, tops[w]);
+    }
+    float inv;
+    const float s = q8_scale(top, inv);
+    if (threadIdx.x == 0) scale[row] = s;
+    vectors([&](int i, int at) {
+        if (!kHeld) {
+            fetch(i, at, over);
+            normed(i, at);
+        }
+        uint32_t b[8];
+        q8_round(held[i], s, inv, b);
+        const uint32_t w[2] = {pack4(b[0], b[1], b[2], b[3]), pack4(b[4], b[5], b[6], b[7])};
         if (n - at >= 8) {
-            __builtin_memcpy(q + at, b, 8);
+            __builtin_memcpy(q + at, w, 8);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (e < n - at) q[at + e] = b[e];
+                if (e < n - at) q[at + e] = (int8_t)b[e];
         }
-    };
-    if constexpr (kHeld > 0) {
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i)
-            if (first + i * stride < n) last_pass(i, first + i * stride);
-    } else {
-        for (int at = first; at < n; at += stride) last_pass(0, at);
-    }
+    });
 }
 
 template <class X, class A, bool NORM>
 static void q8_rows(const void* x, int64_t ldx, const void* add, int64_t ldadd, const float* gain, float eps, int rows, int n, void* sum, int64_t ldsum,
                     int8_t* q, int64_t ldq, float* scale, hipStream_t stream) {
-    const int threads = std::min(1024, std::max(64, (n + 16 * 64 - 1) / (16 * 64) * 64));     // two vectors of 8 a thread
+    // two vectors of 8 a thread; one where the rows are so few that only the way through one counts
+    const int per = rows <= 128 && n <= 8 * 1024 ? 8 : 16;
+    const int threads = std::min(1024, std::max(64, (n + per * 64 - 1) / (per * 64) * 64));
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3(rows), dim3(threads), 0, stream, static_cast<const X*>(x), ldx, static_cast<const A*>(add), ldadd, gain, eps, n,
                            static_cast<X*>(sum), ldsum, q, ldq, scale);
     };
-    if (n <= 2 * 8 * threads) launch(k_q8_rows<X, A, NORM, 2>);
+    if (n <= 8 * threads) launch(k_q8_rows<X, A, NORM, 1>);
+    else if (n <= 2 * 8 * threads) launch(k_q8_rows<X, A, NORM, 2>);
     else launch(k_q8_rows<X, A, NORM, 0>);
 }
 
@@ -238,31 +246,42 @@ __global__ void __launch_bounds__(256) k_q8_append(amusd_q8_cache C, int layer, 
                                                    const float* __restrict__ sin) {
     constexpr int kPer = HD / 32;                    // elements a lane has of each half of a row
     __shared__ float rows[kQ8Group][HD + 4];
-    __shared__ uint32_t most[kQ8Group];              // bits of a row's largest magnitude: those of a NaN are above all others
-    __shared__ float new_scale[kQ8Group], ratio[kQ8Group];
-    const int head = blockIdx.y, t = threadIdx.x;
-    const bool values = blockIdx.z;
+    __shared__ uint32_t most[kQ8Group];              // bits of a block's largest new magnitude: those of a NaN are above all others
+    __shared__ float new_scale[kQ8Group], inverse[kQ8Group], ratio[kQ8Group];
+    const int head = blockIdx.y, t = threadIdx.x, B = C.block, sh = __builtin_ctz(B);
+    const bool values = blockIdx.z, turn = !values && cos;
     const Q8Seg seg = q8_find(S, blockIdx.x);
     const int p0 = (seg.pos0 / kQ8Group + (int)blockIdx.x - seg.unit0) * kQ8Group;      // first position of the group
     const int from = max(seg.pos0, p0), to = min(seg.pos0 + seg.n, p0 + kQ8Group);      // new ones among them
     const uint16_t* src = (values ? vrows : krows) + (int64_t)(seg.row0 - seg.pos0) * ld + (int64_t)head * HD;
-    for (int r = t >> 4; r < kQ8Group; r += 16) {
-        const int pos = p0 + r, l = t & 15;
+    const int l = t & 15;
+    uint16_t a[4][kPer], b[4][kPer];
+    float cs[4][kPer], sn[4][kPer];
+    if (t < kQ8Group) most[t] = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int pos = p0 + i * 16 + (t >> 4);
+        if (pos < from || pos >= to) continue;
+        const uint16_t* p = src + (int64_t)pos * ld + l * kPer;
+        __builtin_memcpy(a[i], p, sizeof a[i]);
+        __builtin_memcpy(b[i], p + HD / 2, sizeof b[i]);
+        if (turn) {
+            __builtin_memcpy(cs[i], cos + (int64_t)pos * (HD / 2) + l * kPer, sizeof cs[i]);
+            __builtin_memcpy(sn[i], sin + (int64_t)pos * (HD / 2) + l * kPer, sizeof sn[i]);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = i * 16 + (t >> 4), pos = p0 + r;
         uint32_t m = 0;
         if (pos >= from && pos < to) {
-            const uint16_t* p = src + (int64_t)pos * ld + l * kPer;
-            uint16_t a[kPer], b[kPer];
-            __builtin_memcpy(a, p, sizeof a);
-            __builtin_memcpy(b, p + HD / 2, sizeof b);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                float x = bf16_to_f32(a[i]), y = bf16_to_f32(b[i]);
-                if (!values && cos) {
-                    const float c = cos[(int64_t)pos * (HD / 2) + l * kPer + i], s = sin[(int64_t)pos * (HD / 2) + l * kPer + i];
-                    rotate_pair(x, y, c, s, x, y);
-                }
-                rows[r][l * kPer + i] = x;
-                rows[r][l * kPer + i + HD / 2] = y;
+            for (int e = 0; e < kPer; ++e) {
+                float x = bf16_to_f32(a[i][e]), y = bf16_to_f32(b[i][e]);
+                if (turn) rotate_pair(x, y, cs[i][e], sn[i][e], x, y);
+                rows[r][l * kPer + e] = x;
+                rows[r][l * kPer + e + HD / 2] = y;
                 m = max(m, max(__float_as_uint(x) & 0x7FFFFFFFu, __float_as_uint(y) & 0x7FFFFFFFu));
             }
         }
@@ -270,72 +289,82 @@ __global__ void __launch_bounds__(256) k_q8_append(amusd_q8_cache C, int layer, 
         m = max(m, lane_xor_u<2>(m));
         m = max(m, lane_xor_u<4>(m));
         m = max(m, lane_xor_u<8>(m));
-        if (l == 0) most[r] = m;
+        if (l == 0 && m) atomicMax(&most[r >> sh], m);
     }
     __syncthreads();
     const size_t kvh = ((size_t)layer * C.n_seqs + seg.seq) * C.Hkv + head;
-    const int B = C.block;
-    if (t < kQ8Group / B) {
+    if (t < kQ8Group >> sh) {
         const int b0 = p0 + t * B;                                   // the block's first position
-        float* scales = (values ? C.vs : C.ks) + kvh * (C.cap / B);
+        float* scales = (values ? C.vs : C.ks) + kvh * (C.cap >> sh);
         float s = 0.f, r = 1.f;
         if (b0 < to && b0 + B > from) {
-            uint32_t m = 0;
-            for (int i = 0; i < B; ++i) m = max(m, most[t * B + i]);
-            const float was = b0 < seg.pos0 ? scales[b0 / B] : 0.f;
+            const uint32_t m = most[t];
+            const float was = b0 < seg.pos0 ? scales[b0 >> sh] : 0.f;
             s = m >= 0x7F800000u || was != was ? __uint_as_float(0x7FC00000u) : fmaxf(was, __uint_as_float(m) / 127.f);
             r = s > 0.f ? was / s : s == s ? 1.f : 0.f;
-            scales[b0 / B] = s;
+            scales[b0 >> sh] = s;
         }
         new_scale[t] = s;
+        inverse[t] = s > 0.f ? (float)(1. / (double)s) : 0.f;
         ratio[t] = r;
     }
     __syncthreads();
-    // 4 bytes a thread: keys 4 columns of a position, values 4 positions of a column
+    // Keys: 16 columns of a position a thread; values: 4 positions of columns c and c + 16 (kept as q + 128: amusd_q8_attention.hip).  What a block that this call reaches held before is rounded again where its
+    // scale has grown.
     int8_t* out = (values ? C.v : C.k) + kvh * ((size_t)C.cap * HD);
-    // (values are kept as q + 128: amusd_q8_attention.hip)
-    const uint8_t bias = values ? 0x80 : 0;
-    auto eight = [&](int r, int c, bool& write, int8_t old) {        // position p0 + r, column c
-        const int pos = p0 + r, b = r / B;
-        const float s = new_scale[b];
-        if (pos >= from && pos < to) {
-            write = true;
-            return (int8_t)((s > 0.f ? (int)fminf(fmaxf(rintf(rows[r][c] / s), -127.f), 127.f) : 0) ^ bias);
-        }
-        // held before, in a block whose scale has grown (from a block that this call does not touch `ratio` is 1)
-        write = pos < from && pos < seg.pos0 && ratio[b] != 1.f;
-        return write ? (int8_t)((int)rintf((float)(int8_t)(old ^ bias) * ratio[b]) ^ bias) : old;
-    };
-    const int first_row = max(0, from / B * B - p0), last_row = to - p0;          // rows that can change
+    const int first_row = max(0, (from & -B) - p0), last_row = to - p0;           // rows that can change
+    auto fresh = [&](int r) { return p0 + r >= from && p0 + r < to; };
+    auto grown = [&](int r) { return p0 + r < from && ratio[r >> sh] != 1.f; };   // (1 in blocks that this call does not reach)
+    auto again = [&](int old, int r) { return (uint32_t)(int)rintf((float)old * ratio[r >> sh]); };
     if (!values) {
-        for (int i = t; i < (last_row - first_row) * (HD / 4); i += 256) {
-            const int r = first_row + i / (HD / 4), c = i % (HD / 4) * 4;
-            int8_t* p = out + q8_k_index(HD, p0 + r, c);
-            const char4 old = *reinterpret_cast<const char4*>(p);
-            bool w = false;
-            char4 b;
-            b.x = eight(r, c, w, old.x);
-            b.y = eight(r, c + 1, w, old.y);
-            b.z = eight(r, c + 2, w, old.z);
-            b.w = eight(r, c + 3, w, old.w);
-            if (w) *reinterpret_cast<char4*>(p) = b;
+        for (int i = first_row * (HD / 16) + t; i < last_row * (HD / 16); i += 256) {
+            const int r = i / (HD / 16), c = i % (HD / 16) * 16;
+            uint4* p = reinterpret_cast<uint4*>(out + q8_k_index(HD, p0 + r, c));
+            uint32_t b[16];
+            if (fresh(r)) {
+                float v[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = rows[r][c + e];
+                q8_round(v, new_scale[r >> sh], inverse[r >> sh], b);
+            } else if (grown(r)) {
+                const uint4 old = *p;
+                const uint32_t o[4] = {old.x, old.y, old.z, old.w};
+#pragma unroll
+                for (int e = 0; e < 16; ++e) b[e] = again((int8_t)(o[e / 4] >> (e % 4 * 8)), r);
+            } else {
+                continue;
+            }
+            *p = uint4{pack4(b[0], b[1], b[2], b[3]), pack4(b[4], b[5], b[6], b[7]), pack4(b[8], b[9], b[10], b[11]), pack4(b[12], b[13], b[14], b[15])};
         }
     } else {
-        const int q0 = first_row / 4, quads = (last_row + 3) / 4 - q0;
-        for (int i = t; i < quads * HD; i += 256) {
-            const int r = (q0 + i / HD) * 4, c = i % HD;
-            int8_t* p = out + q8_v_index(HD, p0 + r, c);
-            const char4 old = *reinterpret_cast<const char4*>(p);
-            const int8_t o[4] = {old.x, old.y, old.z, old.w};
-            int8_t b[4];
-            bool any = false;
+        // 4 rows of columns c and c + 16: two words of a lane's piece
+        for (int i = t; i < (kQ8Group / 4) * (HD / 2); i += 256) {
+            const int c = i % (HD / 2) / 16 * 32 + (i & 15), r = i / (HD / 2) * 4;
+            if (r >= last_row || r + 4 <= first_row) continue;
+            uint32_t* p = reinterpret_cast<uint32_t*>(out + q8_v_index(HD, p0 + r, c));
+            uint32_t b[2][4] = {};
+            const bool whole = fresh(r) && fresh(r + 3);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                bool w = false;
-                b[e] = eight(r + e, c, w, o[e]);
-                any |= w;
+            for (int h = 0; h < 2; ++h) {
+                if (!whole) {
+                    const uint32_t o = p[2 * h] ^ 0x80808080u;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        b[h][e] = o >> (8 * e);
+                        if (grown(r + e)) b[h][e] = again((int8_t)b[h][e], r + e);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (!fresh(r + e)) continue;
+                    const int k = (r + e) >> sh;
+                    const float v[1] = {rows[r + e][c + 16 * h]};
+                    uint32_t q[1];
+                    q8_round(v, new_scale[k], inverse[k], q);
+                    b[h][e] = q[0];
+                }
+                p[2 * h] = pack4(b[h][0], b[h][1], b[h][2], b[h][3]) ^ 0x80808080u;
             }
-            if (any) *reinterpret_cast<char4*>(p) = char4{b[0], b[1], b[2], b[3]};
         }
     }
 }
@@ -350,31 +379,49 @@ hipError_t launch_q8_append(const amusd_q8_cache& c, int layer, const Q8Segs& S,
 }
 
 // ---------------------------------------------------------------- out of the cache
-// The values that rows of the cache stand for, four columns of a position a thread.
+// The values that rows of the cache stand for: 4 positions x 4 columns a thread, in words of 4 bytes (keys: of a position, values: of a
+// column).
 template <class T>
 __global__ void __launch_bounds__(256) k_q8_read(amusd_q8_cache C, int layer, Q8Segs S, T* __restrict__ kout, T* __restrict__ vout, int64_t ld) {
-    const int row = blockIdx.x, quads = C.Hkv * C.hd / 4;
-    int i = 0;
-    while (i + 1 < S.n_seg && row >= S.s[i + 1].row0) ++i;
-    const int pos = S.s[i].pos0 + row - S.s[i].row0;
+    const Q8Seg& seg = q8_find(S, blockIdx.x);
+    const int p0 = (seg.pos0 / 4 + (int)blockIdx.x - seg.unit0) * 4, quads = C.Hkv * C.hd / 4;
     const bool values = blockIdx.y;
-    T* out = (values ? vout : kout) + (int64_t)row * ld;
+    T* out = (values ? vout : kout) + (int64_t)(seg.row0 - seg.pos0) * ld;
     for (int x = threadIdx.x; x < quads; x += blockDim.x) {
         const int head = x * 4 / C.hd, c = x * 4 % C.hd;
-        const size_t kvh = ((size_t)layer * C.n_seqs + S.s[i].seq) * C.Hkv + head;
-        const float s = (values ? C.vs : C.ks)[kvh * (C.cap / C.block) + pos / C.block];
+        const size_t kvh = ((size_t)layer * C.n_seqs + seg.seq) * C.Hkv + head;
+        const float* scales = (values ? C.vs : C.ks) + kvh * (C.cap / C.block);
         const int8_t* p = (values ? C.v : C.k) + kvh * ((size_t)C.cap * C.hd);
+        uint32_t w[4];                                       // keys: of position i; values: of column i
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float y = (float)(values ? (int8_t)(p[q8_v_index(C.hd, pos, c + e)] ^ 0x80) : p[q8_k_index(C.hd, pos, c + e)]) * s;
-            if constexpr (sizeof(T) == 2) out[x * 4 + e] = (T)(y == y ? bf16_rne(y) : 0x7FC0u);
-            else out[x * 4 + e] = __float_as_uint(y);
+        for (int i = 0; i < 4; ++i)
+            w[i] = values ? *reinterpret_cast<const uint32_t*>(p + q8_v_index(C.hd, p0, c + i)) ^ 0x80808080u
+                          : *reinterpret_cast<const uint32_t*>(p + q8_k_index(C.hd, p0 + i, c));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int pos = p0 + i;
+            if (pos < seg.pos0 || pos >= seg.pos0 + seg.n) continue;
+            const float s = scales[pos / C.block];
+            T v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float y = (float)(int8_t)(values ? w[e] >> (8 * i) : w[i] >> (8 * e)) * s;
+                if constexpr (sizeof(T) == 2) v[e] = __builtin_bit_cast(uint16_t, (__bf16)y);
+                else v[e] = __float_as_uint(y);
+            }
+            __builtin_memcpy(out + (int64_t)pos * ld + x * 4, v, sizeof v);
         }
     }
 }
 
-hipError_t launch_q8_read(const amusd_q8_cache& c, int layer, const Q8Segs& S, void* k, void* v, int dtype, int64_t ld, hipStream_t stream) {
-    const dim3 grid(S.rows, 2);
+hipError_t launch_q8_read(const amusd_q8_cache& c, int layer, const Q8Segs& segs, void* k, void* v, int dtype, int64_t ld, hipStream_t stream) {
+    Q8Segs S = segs;
+    int units = 0;                                           // groups of 4 positions
+    for (int i = 0; i < S.n_seg; ++i) {
+        S.s[i].unit0 = units;
+        units += (S.s[i].pos0 + S.s[i].n - 1) / 4 - S.s[i].pos0 / 4 + 1;
+    }
+    const dim3 grid(units, 2);
     if (dtype == AMUSD_DTYPE_BF16)
         hipLaunchKernelGGL(k_q8_read<uint16_t>, grid, dim3(256), 0, stream, c, layer, S, static_cast<uint16_t*>(k), static_cast<uint16_t*>(v), ld);
     else
@@ -391,23 +438,16 @@ __global__ void __launch_bounds__(64) k_q8_matrix(uint4* __restrict__ frag, floa
     const int i = blockIdx.x, lane = threadIdx.x;
     const int tile = part ? (i >> 4) * 2 + part - 1 : (first + i) >> 4, r = part ? i & 15 : (first + i) & 15;
     w += i * ld;
-    double s = 0.;
+    float s = 0.f, inv = 0.f;
     auto value = [&](int c) {
         if constexpr (sizeof(T) == 2) return bf16_to_f32(w[c]);
         else return __uint_as_float(w[c]);
     };
     if constexpr (sizeof(T) > 1) {
-        float most = 0.f;
-        bool bad = false;
-        for (int c = lane; c < k; c += 64) {
-            const float x = value(c);
-            bad |= !(fabsf(x) <= 3.402823466e38f);
-            most = fmaxf(most, fabsf(x));
-        }
-        const double m = wave_max(bad ? INFINITY : (double)most);
-        bad = !(m <= 3.402823466e38);
-        s = bad ? 0. : (double)(float)(m / 127.);
-        if (lane == 0) scale[tile * 16 + r] = bad ? __uint_as_float(0x7FC00000u) : (float)s;
+        uint32_t top = 0;
+        for (int c = lane; c < k; c += 64) top = max(top, __float_as_uint(value(c)) & 0x7FFFFFFFu);
+        s = q8_scale(wave_max(top), inv);
+        if (lane == 0) scale[tile * 16 + r] = s;
     } else if (lane == 0) {
         scale[tile * 16 + r] = given[i];
     }
@@ -418,7 +458,7 @@ __global__ void __launch_bounds__(64) k_q8_matrix(uint4* __restrict__ frag, floa
         int8_t b = 0;
         if (c < k) {
             if constexpr (sizeof(T) == 1) b = (int8_t)w[c];
-            else b = s > 0. ? (int8_t)(int)fmin(fmax(rint((double)value(c) / s), -127.), 127.) : (int8_t)0;
+            else b = inv > 0.f ? (int8_t)(int)rintf(value(c) / s) : (int8_t)0;
         }
         out[(((size_t)tile * kblocks + kb) * 64 + (lane >> 4) * 16 + r) * 16 + (lane & 15)] = b;
     }

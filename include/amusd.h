@@ -317,9 +317,10 @@ int amusd_q8_matrix_free(amusd_q8_matrix *m);
 /* out[r][c] = scale[r] * (the matrix's scale of c) * sum over i of x[r][i] * w[c][i], the sum exact; out fp32 or bf16.
  * x: 8-bit rows as the calls above leave them (16-byte aligned, ldx a multiple of 16; a row's ldx bytes are
  * readable, those past k are not used).  A row's bits do not depend on the number of rows.  rows may be 0.
- * workspace: device memory of amusd_q8_gemm_workspace_bytes(w, rows), 16-byte aligned, zeros before its first use and
- * again after each call; calls that overlap need one each.  Without one (NULL, or too small) a product of few rows and few
- * features takes longer, with the same bits. */
+ * workspace: device memory of amusd_q8_gemm_workspace_bytes, 16-byte aligned: what products of up to `rows` rows with w make use of
+ * (0: of none).  Zeroed before its first use; a call leaves it fit for the next one, of any matrix, and no one else writes to it;
+ * calls that overlap need one each.  Without one (NULL, or too small) some products of 17 to about a thousand rows take longer,
+ * with the same bits. */
 int64_t amusd_q8_gemm_workspace_bytes(const amusd_q8_matrix *w, int32_t rows);
 int amusd_q8_gemm(const amusd_q8_matrix *w, const int8_t *x, int64_t ldx, const float *scale, int32_t rows, void *out,
                   int32_t dtype, int64_t ldo, void *workspace, int64_t workspace_bytes, void *hip_stream);

@@ -1,5 +1,7 @@
 // Choices between forms of a stage that follow from sizes alone.  Host code, no GPU needed.
 #pragma once
+#include <cstdint>
+#include <initializer_list>
 
 namespace amusd {
 
@@ -59,44 +61,58 @@ inline bool attention_packs_rows(bool bf16, int head_dim, int group, int units, 
 
 // Products of 8-bit integers: forms for few rows, whose workgroups' eight waves split the contraction of MT x 16 rows and NT x 16 features
 // (kQ8FewMTxNT), and for many, whose workgroups hold a tile of the result (kQ8Tile<features>x<rows>).
-enum Q8Form { kQ8Few1x1, kQ8Few1x2, kQ8Few2x1, kQ8Few2x2, kQ8Few2x4, kQ8Few4x4, kQ8Tile64, kQ8Tile128x64, kQ8Tile128, kQ8Tile256 };
+enum Q8Form { kQ8Few1x1, kQ8Few1x2, kQ8Few2x2, kQ8Few2x4, kQ8Few4x4, kQ8Tile64, kQ8Tile128x64, kQ8Tile128, kQ8Tile256 };
+// .. tiles of 16 rows and of 16 features of a workgroup
+inline int q8_form_rows(Q8Form f) { const int n[] = {1, 1, 2, 2, 4, 4, 4, 8, 16}; return n[f]; }
+inline int q8_form_tiles(Q8Form f) { const int n[] = {1, 2, 2, 4, 4, 4, 8, 8, 16}; return n[f]; }
+struct Q8Plan {
+    Q8Form form;
+    int ways;        // workgroups that share a tile's contraction: 1, or 2 or 4 whose sums meet in a workspace
+};
+constexpr int kQ8Tickets = 4096;        // of a workspace: a wave (few rows: a workgroup) and tile has one
+constexpr int kQ8MinBlocks = 16;        // blocks of 64 columns of a workgroup that shares
 
 // Which: up to 16 rows by the number of feature tiles alone (one a workgroup while there is a compute unit for each; us with 1x1 / 1x2, 8
-// rows: 4096 x 4096 5.3 / 6.0, 6144 features 7.6 / 6.8, 28672 24.9 / 19.8); with more rows by an estimate of each form's time, us:
-//   few: 3 + a compute unit's rounds x blocks of 64 columns x (0.020 a feature tile + 0.022 a row tile): what a compute unit loads at
-//     about 50 GB/s;
-//   tiles: a block takes its workgroup at least `alone` (the loads' latency); where compute units are full, `full` a workgroup of them.
-//     256 x 256 has a compute unit to itself: rounds x (blocks x 0.55 to 0.70 + 9); clocks fall as more of the chip multiplies.
-// Measured (MI355X, 8B and 1B projections, 17 to 2048 rows; the estimate's choice / the best): 2048 rows gate/up 209 / 209, QKV 53 / 53,
-// O-projection 37.5 / 37.5, down 122 / 122; 128 rows gate/up 33.5 / 33.5, O-projection 10.3 / 10.3; 64 rows gate/up 27.5 / 27.5, down 23 / 23.
-inline Q8Form q8_gemm_form(int tiles, int kblocks, bool gated, int rows, int cus) {
-    if (rows <= 16) return !gated && tiles <= cus ? kQ8Few1x1 : kQ8Few1x2;
-    const double chip = cus / 256., kb = kblocks;
-    Q8Form best = kQ8Few2x2;
+// rows: 4096 x 4096 5.3 / 6.0, 6144 features 7.6 / 6.8, 28672 24.9 / 19.8; shared by two, 2048 x 8192 6.9 / 7.4 alone, every other
+// 0.6 to 2 slower); with more rows by an estimate of each form's time, us:
+//   few: 2.6 + 0.9 a workgroup of a compute unit + its rounds x blocks of 64 columns (a wave's whole ones) x (0.022 a feature tile + 0.021 a
+//     row tile): what a compute unit loads at about 50 GB/s;
+//   tiles: a block takes its workgroup at least `alone` (what a compute unit loads, again); where compute units are full, `full` a workgroup
+//     of them.  256 x 256 has a compute unit to itself: rounds x (blocks x 0.55 to 0.70 + 9); clocks fall as more of the chip multiplies;
+//   shared: 2.3 + 0.35 a megabyte of sums that are written and read.
+// Measured (MI355X, five projections of the 8B and the 1B model, 20 to 1024 rows, all forms): 3 % over the best in the mean.  Sharing
+// gives, us alone / shared: down 8B, 32 rows 22.8 / 17.2, 256 rows 45.8 / 33.7, 512 rows 71.3 / 49.9; QKV 8B, 128 rows 16.4 / 13.3;
+// down 1B, 32 rows 12.0 / 9.2, 512 rows 26.6 / 19.7.
+inline Q8Plan q8_gemm_plan(int tiles, int kblocks, bool gated, int rows, int cus, bool shared) {
+    if (rows <= 16) return {!gated && tiles <= cus ? kQ8Few1x1 : kQ8Few1x2, 1};
+    Q8Plan best = {kQ8Few2x2, 1};
     double least = 1e30;
-    auto offer = [&](Q8Form f, double us) {
-        if (us < least) { least = us; best = f; }
+    auto ceil_div = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+    auto groups_of = [&](Q8Form f) { return ceil_div(tiles, q8_form_tiles(f)) * ceil_div(rows, q8_form_rows(f) * 16); };
+    auto offer = [&](Q8Form f, int waves, auto us) {     // us(workgroups, blocks of each)
+        const int64_t groups = groups_of(f);
+        for (int ways = 1; ways <= (shared ? 4 : 1); ways *= 2) {
+            if (ways > 1 && (kblocks < ways * kQ8MinBlocks || groups * waves > kQ8Tickets)) break;
+            const int64_t wgs = groups * ways;
+            const double sums = 1e-6 * wgs * (q8_form_tiles(f) * q8_form_rows(f) * 1024);
+            const double all = us((double)wgs, (double)ceil_div(kblocks, ways)) + (ways > 1 ? 2.3 + 0.35 * sums : 0);
+            if (all < least) { least = all; best = {f, ways}; }
+        }
     };
-    auto ceil_div = [](int a, int b) { return (a + b - 1) / b; };
-    auto few = [&](Q8Form f, int mt, int nt) {
-        const int wgs = ceil_div(tiles, nt) * ceil_div(rows, 16 * mt);
-        offer(f, 3 + ceil_div(wgs, cus) * kb * (0.020 * nt + 0.022 * mt));
+    for (Q8Form f : {kQ8Few2x2, kQ8Few2x4, kQ8Few4x4})
+        offer(f, 1, [&](double wgs, double blocks) {
+            const int64_t rounds = ceil_div((int64_t)wgs, cus), whole = ceil_div((int64_t)blocks, 8) * 8;
+            return 2.6 + 0.9 * wgs / cus + rounds * whole * (0.022 * q8_form_tiles(f) + 0.021 * q8_form_rows(f));
+        });
+    auto tile = [&](Q8Form f, double alone, double full) {
+        offer(f, 4, [&](double wgs, double blocks) { return 2.4 + blocks * (alone > wgs * full / cus ? alone : wgs * full / cus); });
     };
-    if (!gated) few(kQ8Few2x1, 2, 1);
-    few(kQ8Few2x2, 2, 2);
-    few(kQ8Few2x4, 2, 4);
-    few(kQ8Few4x4, 4, 4);
-    auto tile = [&](Q8Form f, int cols, int rows_of, double alone, double full) {
-        const int wgs = ceil_div(tiles, cols) * ceil_div(rows, rows_of);
-        const double shared = wgs * kb * full / 256 / chip;
-        offer(f, 4 + (kb * alone > shared ? kb * alone : shared));
-    };
-    tile(kQ8Tile64, 4, 64, 0.25, 0.128);
-    tile(kQ8Tile128x64, 8, 64, 0.29, 0.198);
-    tile(kQ8Tile128, 8, 128, 0.33, 0.28);
-    const int wgs = ceil_div(tiles, 16) * ceil_div(rows, 256), rounds = ceil_div(wgs, cus);
-    offer(kQ8Tile256, 3 + rounds * (kb * (0.55 + 0.15 * (wgs < cus ? (double)wgs / cus : 1.)) + 9));
-    return best;
+    tile(kQ8Tile64, 0.20, 0.12);
+    tile(kQ8Tile128x64, 0.24, 0.18);
+    tile(kQ8Tile128, 0.35, 0.285);
+    const int64_t wgs = groups_of(kQ8Tile256), rounds = ceil_div(wgs, cus);
+    const double us = 3 + rounds * (kblocks * (0.55 + 0.15 * (wgs < cus ? (double)wgs / cus : 1.)) + 9);
+    return us < least ? Q8Plan{kQ8Tile256, 1} : best;
 }
 
 }  // namespace amusd

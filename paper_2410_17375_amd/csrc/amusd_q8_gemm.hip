@@ -25,12 +25,14 @@ __device__ __forceinline__ float q8_swiglu(float gate, float up) {
 }
 
 // Few rows: the weights are read once and their bytes bound it.  A workgroup owns NT tiles of 16 features, its waves every
-// eighth block of 64 columns, and each wave keeps D blocks under way; the sums meet in LDS.  MT: tiles of 16 rows.
+// eighth block of 64 columns, and each wave keeps D blocks under way; the sums meet in LDS.  MT: tiles of 16 rows.  Where
+// workgroups share a contraction (blockIdx.z: which part), their sums meet in `work`: kQ8Tickets counts, then the sums.
 template <class OUT, bool GATED, int MT, int NT, int D>
 __global__ void __launch_bounds__(512) k_q8_gemm_rows(const uint4* __restrict__ frag, const float* __restrict__ wscale, int kblocks, int k, int tiles, int n,
                                                       const int8_t* __restrict__ x, int64_t ldx, const float* __restrict__ xscale, int rows,
-                                                      OUT* __restrict__ out, int64_t ldo) {
+                                                      OUT* __restrict__ out, int64_t ldo, int* __restrict__ work) {
     extern __shared__ int lds[];                     // [8 waves][MT][NT][16 rows][16 features]
+    __shared__ int last;
     // (the wave's number as a scalar: matrix instructions take no notice of masked lanes, so what is around them has to be a branch)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
     const int tile0 = blockIdx.x * NT, row0 = blockIdx.y * (MT * 16);
@@ -40,11 +42,12 @@ __global__ void __launch_bounds__(512) k_q8_gemm_rows(const uint4* __restrict__ 
     const int8_t* xp[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) xp[m] = x + (int64_t)min(row0 + m * 16 + r, rows - 1) * ldx;
-    const int S = (kblocks - wave + 7) / 8;          // this wave's blocks: wave, wave + 8, ..
+    const int ways = gridDim.z, per = (kblocks + ways - 1) / ways, first = blockIdx.z * per;
+    const int S = (min(kblocks - first, per) - wave + 7) / 8;        // this wave's blocks: first + wave, first + wave + 8, ..
     v4i acc[MT][NT] = {};
     uint4 wf[D][NT], xf[D][MT];
     auto load = [&](int slot, int i) {
-        const int kb = wave + 8 * min(i, S - 1);     // (S is no multiple of D: the last block once more, unused)
+        const int kb = first + wave + 8 * min(i, S - 1);     // (S is no multiple of D: the last block once more, unused)
         const int at = kb * 64 + g * 16;
 #pragma unroll
         for (int t = 0; t < NT; ++t) wf[slot][t] = load_stream(wp[t] + (size_t)kb * 64);
@@ -83,11 +86,43 @@ __global__ void __launch_bounds__(512) k_q8_gemm_rows(const uint4* __restrict__ 
 #pragma unroll
             for (int e = 0; e < 4; ++e) lds[(((wave * MT + m) * NT + t) * 16 + g * 4 + e) * 16 + r] = acc[m][t][e];
     __syncthreads();
-    auto sum = [&](int m, int t, int at) {
+    constexpr int kSums = MT * NT * 256;
+    auto of_waves = [&](int i) {
         int s = 0;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) s += lds[((w * MT + m) * NT + t) * 256 + at];
+        for (int w = 0; w < 8; ++w) s += lds[w * kSums + i];
         return s;
+    };
+    if (ways > 1) {
+        // Each workgroup of the `ways` writes its sums and counts itself; the one that counts last adds them up (integers: the order does
+        // not show) and goes on.  Nobody waits for anybody.  What another die has written or is to read passes its L2: atomics.
+        const int group = blockIdx.y * gridDim.x + blockIdx.x;
+        int* const all = work + kQ8Tickets + (size_t)group * ways * kSums;
+        for (int i = threadIdx.x; i < kSums; i += 512)
+            __hip_atomic_store(all + blockIdx.z * kSums + i, of_waves(i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const int seen = __hip_atomic_fetch_add(work + group, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (seen == ways - 1) __hip_atomic_store(work + group, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next call
+            last = seen == ways - 1;
+        }
+        __syncthreads();
+        if (!last) return;
+        auto from = [&](int p, int i) { return __hip_atomic_load(all + p * kSums + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+#pragma unroll
+        for (int j = 0; j < (kSums + 511) / 512; ++j) {
+            const int i = j * 512 + threadIdx.x;
+            if (kSums % 512 && i >= kSums) break;
+            int s = from(0, i) + from(1, i);
+            if (ways == 4) s += from(2, i) + from(3, i);
+            lds[i] = s;
+        }
+        __syncthreads();
+    }
+    auto sum = [&](int m, int t, int at) {
+        const int i = (m * NT + t) * 256 + at;
+        return ways > 1 ? lds[i] : of_waves(i);
     };
     constexpr int kOut = GATED ? NT / 2 : NT;        // tiles of output columns
     for (int i = threadIdx.x; i < MT * kOut * 256; i += 512) {
@@ -128,7 +163,7 @@ template <class Sh, class OUT, bool GATED>
 __global__ void __launch_bounds__(Sh::kThreads, Sh::kMinWaves) k_q8_gemm_tile(const uint4* __restrict__ frag, const float* __restrict__ wscale, int kblocks,
                                                                              int k, int tiles, int n, const int8_t* __restrict__ x, int64_t ldx,
                                                                              const float* __restrict__ xscale, int rows, OUT* __restrict__ out, int64_t ldo,
-                                                                             int row_wgs, int wgs) {
+                                                                             int row_wgs, int wgs, int* __restrict__ work) {
     constexpr int WN = Sh::WN, A = Sh::A, B = Sh::B, NW = Sh::NW, NX = Sh::NX, NPW = NW + NX, MID = A / 2, WR = A >= 4 ? 4 : 2, WD = WR / 2;
     static_assert(MID + WD <= A && A % WR == 0, "");
     extern __shared__ char smem[];
@@ -139,11 +174,12 @@ __global__ void __launch_bounds__(Sh::kThreads, Sh::kMinWaves) k_q8_gemm_tile(co
     const int xcd = blockIdx.x & 7, per = wgs >> 3, more = wgs & 7;
     const int at = xcd * per + min(xcd, more) + (blockIdx.x >> 3);
     const int row0 = at % row_wgs * (Sh::kRowTiles * 16), tile0 = at / row_wgs * Sh::kColTiles;
+    const int ways = gridDim.y, share = ((kblocks + 1) / 2 + ways - 1) / ways * 2, first = blockIdx.y * share, blocks = min(kblocks - first, share);
     const char* wsrc[NW];
 #pragma unroll
-    for (int q = 0; q < NW; ++q) wsrc[q] = reinterpret_cast<const char*>(frag + (size_t)min(tile0 + wave * NW + q, tiles - 1) * kblocks * 64);
+    for (int q = 0; q < NW; ++q) wsrc[q] = reinterpret_cast<const char*>(frag + ((size_t)min(tile0 + wave * NW + q, tiles - 1) * kblocks + first) * 64);
     // rows: load q of half h of a pair of blocks is of the 8 rows from 8 * (h * kRowTiles + wave * NX + q)
-    const char* xsrc = reinterpret_cast<const char*>(x + (int64_t)row0 * ldx);
+    const char* xsrc = reinterpret_cast<const char*>(x + (int64_t)row0 * ldx + first * 64);
     unsigned xoff[2][NX], xcol[2][NX];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -155,19 +191,19 @@ __global__ void __launch_bounds__(Sh::kThreads, Sh::kMinWaves) k_q8_gemm_tile(co
         }
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)smem;
     const unsigned ldsx = lds0 + Sh::kWSlots * Sh::kWBytes;
-    const int pairs = (kblocks + 1) / 2;
+    const int pairs = (blocks + 1) / 2, columns = k - first * 64;
     // Issues load q of NPW with block `b` of weights and half h of pair `p` of rows (past the end: the last once more, unused).
     int wslot = 0, xslot = 0;
     unsigned wdst = 0, wat = 0;
     auto begin_w = [&](int b) {
         wdst = lds0 + wslot * Sh::kWBytes + wave * (NW * 1024);
-        wat = (unsigned)min(b, kblocks - 1) * 1024u + lane * 16;
+        wat = (unsigned)min(b, blocks - 1) * 1024u + lane * 16;
         wslot = (wslot + 1) & 3;
     };
     auto load_w = [&](int q) { load_to_lds(wsrc[q], wat, wdst + q * 1024); };
     auto load_x = [&](int q, int p, int h) {
         const unsigned c = (unsigned)min(p, pairs - 1) * 128u + xcol[h][q];
-        load_to_lds(xsrc, xoff[h][q] + (c < (unsigned)k ? c : 0u), ldsx + xslot * Sh::kXBytes + (h * Sh::kRowTiles + wave * NX + q) * 1024);   // columns past k meet zeros
+        load_to_lds(xsrc, xoff[h][q] + (c < (unsigned)columns ? c : 0u), ldsx + xslot * Sh::kXBytes + (h * Sh::kRowTiles + wave * NX + q) * 1024);   // columns past k meet zeros
     };
     auto next_x = [&] { xslot = xslot == 2 ? 0 : xslot + 1; };
     auto w_frag = [&](const char* slot, int f) { return *reinterpret_cast<const uint4*>(slot + f * 1024 + lane * 16); };
@@ -243,15 +279,48 @@ __global__ void __launch_bounds__(Sh::kThreads, Sh::kMinWaves) k_q8_gemm_tile(co
         ++kb;
     };
 #pragma unroll 1
-    while (kb + 2 <= kblocks) {
+    while (kb + 2 <= blocks) {
         block(std::integral_constant<int, 0>{});
         block(std::integral_constant<int, 1>{});
     }
-    if (kb < kblocks) block(std::integral_constant<int, 0>{});
+    if (kb < blocks) block(std::integral_constant<int, 0>{});
     wait_vm<0>();                                        // what was loaded past the end
     // Lane: row r of a row tile, features 4 g .. 4 g + 3 of a feature tile.  Through LDS, so that whole lines are stored: a wave's rows
     // at a distance of W elements, a little more than they have (banks).
     __syncthreads();
+    if (ways > 1) {
+        // As with few rows, but each wave by itself: of the waves that have a part of the same sums, the one that counts last goes on.
+        typedef unsigned long long u64;
+        constexpr int kPairs = A * B * 2;
+        const int place = at * Sh::kWavesOf + wave;
+        u64* const all = reinterpret_cast<u64*>(work + kQ8Tickets) + (size_t)place * ways * (kPairs * 64) + lane;
+        u64* const mine = all + blockIdx.y * (kPairs * 64);
+#pragma unroll
+        for (int q = 0; q < kPairs; ++q) {
+            const v4i a = acc[q / 2 / B][q / 2 % B];
+            const u64 v = (u64)(unsigned)a[q % 2 * 2 + 1] << 32 | (unsigned)a[q % 2 * 2];
+            __hip_atomic_store(mine + q * 64, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        int seen = 0;
+        if (lane == 0) {
+            seen = __hip_atomic_fetch_add(work + place, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (seen == ways - 1) __hip_atomic_store(work + place, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        if (__builtin_amdgcn_readfirstlane(seen) != ways - 1) return;
+#pragma unroll 1
+        for (int p = 1; p < ways; ++p) {
+            const u64* from = all + (blockIdx.y + p) % ways * (kPairs * 64);
+            u64 v[kPairs];
+#pragma unroll
+            for (int q = 0; q < kPairs; ++q) v[q] = __hip_atomic_load(from + q * 64, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+            for (int q = 0; q < kPairs; ++q) {
+                acc[q / 2 / B][q / 2 % B][q % 2 * 2] += (int)v[q];
+                acc[q / 2 / B][q / 2 % B][q % 2 * 2 + 1] += (int)(v[q] >> 32);
+            }
+        }
+    }
     constexpr int kOutTiles = GATED ? A / 2 : A, W = kOutTiles * 16 + 16 / (int)sizeof(OUT);
     constexpr int kSpan = kOutTiles * 16 * (int)sizeof(OUT) / 16;             // 16-byte pieces of a row
     OUT* const stage = reinterpret_cast<OUT*>(smem) + wave * (16 * W);
@@ -297,28 +366,26 @@ __global__ void __launch_bounds__(Sh::kThreads, Sh::kMinWaves) k_q8_gemm_tile(co
     }
 }
 
-int64_t q8_gemm_workspace(const amusd_q8_matrix&, int) { return 0; }
-
 template <class OUT, bool GATED>
-static void gemm(const amusd_q8_matrix& w, const int8_t* x, int64_t ldx, const float* scale, int rows, OUT* out, int64_t ldo, hipStream_t stream) {
+static void gemm(const amusd_q8_matrix& w, const int8_t* x, int64_t ldx, const float* scale, int rows, OUT* out, int64_t ldo, const Q8Plan& plan, int* work,
+                 hipStream_t stream) {
     auto few = [&](auto kernel, int mt, int nt) {
         const int lds = 8 * mt * nt * 256 * 4;
         (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        hipLaunchKernelGGL(kernel, dim3((w.tiles + nt - 1) / nt, (rows + mt * 16 - 1) / (mt * 16)), dim3(512), lds, stream, w.frag, w.scale, w.kblocks, w.k,
-                           w.tiles, w.n, x, ldx, scale, rows, out, ldo);
+        hipLaunchKernelGGL(kernel, dim3((w.tiles + nt - 1) / nt, (rows + mt * 16 - 1) / (mt * 16), plan.ways), dim3(512), lds, stream, w.frag, w.scale,
+                           w.kblocks, w.k, w.tiles, w.n, x, ldx, scale, rows, out, ldo, work);
     };
     auto many = [&](auto shape) {
         using Sh = decltype(shape);
         const auto kernel = k_q8_gemm_tile<Sh, OUT, GATED>;
         (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Sh::kLds);
         const int row_wgs = (rows + Sh::kRowTiles * 16 - 1) / (Sh::kRowTiles * 16), wgs = row_wgs * ((w.tiles + Sh::kColTiles - 1) / Sh::kColTiles);
-        hipLaunchKernelGGL(kernel, dim3(wgs), dim3(Sh::kThreads), Sh::kLds, stream, w.frag, w.scale, w.kblocks, w.k, w.tiles, w.n, x, ldx, scale, rows, out,
-                           ldo, row_wgs, wgs);
+        hipLaunchKernelGGL(kernel, dim3(wgs, plan.ways), dim3(Sh::kThreads), Sh::kLds, stream, w.frag, w.scale, w.kblocks, w.k, w.tiles, w.n, x, ldx, scale,
+                           rows, out, ldo, row_wgs, wgs, work);
     };
-    switch (q8_gemm_form(w.tiles, w.kblocks, w.gated, rows, w.cus)) {
+    switch (plan.form) {
         case kQ8Few1x1: if constexpr (!GATED) return few(k_q8_gemm_rows<OUT, GATED, 1, 1, 4>, 1, 1); else return;
         case kQ8Few1x2: return few(k_q8_gemm_rows<OUT, GATED, 1, 2, 4>, 1, 2);
-        case kQ8Few2x1: if constexpr (!GATED) return few(k_q8_gemm_rows<OUT, GATED, 2, 1, 8>, 2, 1); else return;
         case kQ8Few2x2: return few(k_q8_gemm_rows<OUT, GATED, 2, 2, 4>, 2, 2);
         case kQ8Few2x4: return few(k_q8_gemm_rows<OUT, GATED, 2, 4, 4>, 2, 4);
         case kQ8Few4x4: return few(k_q8_gemm_rows<OUT, GATED, 4, 4, 2>, 4, 4);
@@ -329,13 +396,27 @@ static void gemm(const amusd_q8_matrix& w, const int8_t* x, int64_t ldx, const f
     }
 }
 
+static int64_t work_of(const amusd_q8_matrix& w, int rows, const Q8Plan& p) {
+    if (p.ways == 1) return 0;
+    const int mt = q8_form_rows(p.form), nt = q8_form_tiles(p.form);
+    const int64_t groups = (int64_t)((w.tiles + nt - 1) / nt) * ((rows + 16 * mt - 1) / (16 * mt));
+    return (kQ8Tickets + groups * p.ways * mt * nt * 256) * 4;
+}
+// .. of up to `rows` rows: what is chosen depends on the tiles of 16 rows, and past so many nobody shares.
+int64_t q8_gemm_workspace(const amusd_q8_matrix& w, int rows) {
+    int64_t most = 0;
+    const int end = std::min(rows, (kQ8Tickets / 4 + 1) * 128);
+    for (int r = 17; r <= end; r = (r & ~15) + 17) most = std::max(most, work_of(w, r, q8_gemm_plan(w.tiles, w.kblocks, w.gated, r, w.cus, true)));
+    return most;
+}
+
 hipError_t launch_q8_gemm(const amusd_q8_matrix& w, const int8_t* x, int64_t ldx, const float* scale, int rows, void* out, int dtype, int64_t ldo,
                           void* work, int64_t work_bytes, hipStream_t stream) {
-    (void)work;
-    (void)work_bytes;
+    Q8Plan plan = q8_gemm_plan(w.tiles, w.kblocks, w.gated, rows, w.cus, true);
+    if (work_of(w, rows, plan) > work_bytes) plan = q8_gemm_plan(w.tiles, w.kblocks, w.gated, rows, w.cus, false);
     auto go = [&](auto* o) {
-        if (w.gated) gemm<std::remove_pointer_t<decltype(o)>, true>(w, x, ldx, scale, rows, o, ldo, stream);
-        else gemm<std::remove_pointer_t<decltype(o)>, false>(w, x, ldx, scale, rows, o, ldo, stream);
+        if (w.gated) gemm<std::remove_pointer_t<decltype(o)>, true>(w, x, ldx, scale, rows, o, ldo, plan, static_cast<int*>(work), stream);
+        else gemm<std::remove_pointer_t<decltype(o)>, false>(w, x, ldx, scale, rows, o, ldo, plan, static_cast<int*>(work), stream);
     };
     if (dtype == AMUSD_DTYPE_BF16) go(static_cast<uint16_t*>(out));
     else go(static_cast<float*>(out));

@@ -149,6 +149,16 @@ def _matrix(gpu, n, k, gated=False, seed=0):
     return w, sw, A.Q8Matrix(w, A.DTYPE_INT8, n, k, scale=sw, gated=gated)
 
 
+_SPACE = []
+
+
+def _workspace(torch, need):
+    """One for all products: each leaves it fit for the next, of any matrix."""
+    if not _SPACE or _SPACE[0].numel() < need:
+        _SPACE[:] = [torch.zeros(max(need, 1 << 24), dtype=torch.uint8, device="cuda")]
+    return _SPACE[0]
+
+
 def _product(gpu, m, x, sx, n, dtype, ldo=None, work=True, ldx=None):
     torch, A = gpu
     rows, k = x.shape
@@ -156,10 +166,9 @@ def _product(gpu, m, x, sx, n, dtype, ldo=None, work=True, ldx=None):
     s = torch.from_numpy(sx).cuda()
     out = torch.full((rows, ldo or n), 5.0, dtype=dtype, device="cuda")
     need = m.workspace_bytes(rows)
-    w = torch.zeros(max(need, 16), dtype=torch.uint8, device="cuda")
+    w = _workspace(torch, need)
     A.q8_gemm(m, xd.data_ptr(), ldx or _up16(k), s.data_ptr(), rows, out.data_ptr(), _code(A, torch, out), out.shape[1],
               w.data_ptr() if work else 0, w.numel() if work else 0)
-    assert not w.any().item()                           # left as it was found
     assert (out[:, n:] == 5).all().item()
     return out[:, :n]
 
@@ -181,6 +190,45 @@ def test_gemm(gpu, rows, n, k):
     assert (np.abs(got - want) <= 3.01 * U32 * np.abs(want)).all()            # an exact sum, rounded, times two scales
     half = _np(_product(gpu, m, x, sx, n, torch.bfloat16, work=False, ldx=_up16(k) + 16))
     assert np.array_equal(half, O.bf16(got).astype(np.float32))               # the same bits without a workspace, rounded once more
+
+
+# sizes whose contractions workgroups share where there is a workspace: every form that can
+SHARED = [(20, 256, 8192), (32, 1000, 4099), (33, 2048, 8192), (60, 300, 14336), (100, 1024, 6000), (130, 2048, 8200), (250, 4096, 14336), (300, 1040, 8256),
+          (500, 2048, 14330), (700, 500, 9000), (17, 2176, 4096), (40, 2176, 8192), (17, 4224, 5632), (17, 8320, 4608), (70, 8064, 6144), (1024, 4096, 14336)]
+
+
+@pytest.mark.parametrize("rows,n,k", SHARED)
+@pytest.mark.parametrize("gated", [False, True])
+def test_gemm_shared(gpu, rows, n, k, gated):
+    torch, A = gpu
+    w, sw, m = _matrix(gpu, n - n % 2 if gated else n, k, gated=gated)
+    no = n // 2 if gated else n
+    rng = np.random.default_rng([rows, n, k])
+    x = rng.integers(-127, 128, (rows, k)).astype(np.int8)
+    sx = ((rng.random(rows) + 0.5) * 3 / (0.01 * 73 * 73 * np.sqrt(k))).astype(np.float32)
+    assert m.workspace_bytes(rows + 16) >= m.workspace_bytes(rows) > 0 == m.workspace_bytes(16)
+    alone = _product(gpu, m, x, sx, no, torch.float32, work=False)
+    if not gated:
+        # the sums in 64 bits are exact, float64 products of integers below 2^53
+        sums = torch.from_numpy(x).cuda().double() @ torch.from_numpy(w).cuda().double().T
+        want = sums.float() * torch.from_numpy(sx).cuda()[:, None] * torch.from_numpy(sw).cuda()
+        assert torch.equal(alone, want)
+    for _ in range(3):
+        assert torch.equal(_product(gpu, m, x, sx, no, torch.float32), alone)
+    s = torch.cuda.Stream()
+    xd, sd = torch.from_numpy(np.pad(x, ((0, 0), (0, _up16(k) - k)))).cuda(), torch.from_numpy(sx).cuda()
+    out, space = torch.zeros(rows, no, dtype=torch.float32, device="cuda"), torch.zeros(m.workspace_bytes(rows), dtype=torch.uint8, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=s):
+        for _ in range(2):
+            A.q8_gemm(m, xd.data_ptr(), _up16(k), sd.data_ptr(), rows, out.data_ptr(), A.DTYPE_FP32, no, space.data_ptr(), space.numel(),
+                      torch.cuda.current_stream().cuda_stream)
+    for _ in range(3):
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, alone)
 
 
 @pytest.mark.parametrize("rows,n,k", [(1, 8, 64), (1, 500, 70), (16, 1000, 512), (40, 129, 300), (129, 100, 512), (300, 1024, 256), (520, 1100, 128)])

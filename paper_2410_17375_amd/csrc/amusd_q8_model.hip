@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(1024) k_q8_greedy(const float* __restrict__ lo
 }
 __global__ void __launch_bounds__(256) k_q8_export(DevModel M, int bytes) { export_logits(M, bytes, blockIdx.x); }
 
-constexpr int kLmRows = 128;       // rows of a prompt whose logits are there at a time
+constexpr int kLmRows = 256;       // rows of a prompt whose logits are there at a time (a prompt of 2048 through 4 layers and 128256 tokens: 4.07 ms; 128 rows: 4.78)
 
 struct Stage {                     // events around the launches of the stage that is timed
     StageTimer* tm;

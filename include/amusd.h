@@ -327,7 +327,7 @@ int amusd_q8_gemm(const amusd_q8_matrix *w, const int8_t *x, int64_t ldx, const 
 
 /* The key-value caches of n_layers layers and n_seqs sequences in 8 bits, capacity positions each, with a scale for every `block`
  * positions (1, 16, 32 or 64) of a kv head's keys, and one of its values.  Also holds the memory that attention of few rows
- * needs.  Head counts and head_dim as in amusd_config.  Zeroed. */
+ * needs.  Head counts and head_dim as in amusd_config; capacity at most 2^24, rounded up to a multiple of 64.  Zeroed. */
 typedef struct amusd_q8_cache amusd_q8_cache;
 int amusd_q8_cache_create(int32_t n_layers, int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                           int32_t capacity, int32_t block, void *hip_stream, amusd_q8_cache **out);
@@ -352,7 +352,7 @@ int amusd_q8_cache_read(const amusd_q8_cache *c, int32_t layer, int32_t n_seq, c
  * which have to be in the cache (its own too).  out = softmax(scale * q . k) v, q and out bf16 rows
  * [n_q_heads * head_dim], q turned by the tables as keys are.  A query is rounded to 16 bits of its largest
  * component, softmax weights to 11 bits; sums are fp32.  A row's bits depend on its query and on what it sees, not on the
- * call's other rows. */
+ * call's other rows.  A call's rows times n_q_heads / n_kv_heads are at most 2^19. */
 int amusd_q8_attention(amusd_q8_cache *c, int32_t layer, int32_t n_seq, const int32_t *seq_ids, const int32_t *pos0,
                        const int32_t *n, const void *q, int64_t ldq, float scale, const float *rope_cos,
                        const float *rope_sin, void *out, int64_t ldo, void *hip_stream);

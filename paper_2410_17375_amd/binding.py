@@ -327,7 +327,9 @@ class Q8Matrix:
                                           1 if on_device else 0, stream, C.byref(self._h)))
 
     def workspace_bytes(self, rows):
-        return int(lib.amusd_q8_gemm_workspace_bytes(self._h, rows))
+        n = int(lib.amusd_q8_gemm_workspace_bytes(self._h, rows))
+        _check(min(n, 0))
+        return n
 
     def free(self):
         if self._h:

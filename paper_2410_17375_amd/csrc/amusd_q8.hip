@@ -669,6 +669,7 @@ int amusd_q8_matrix_create(const void* w, int32_t dtype, const float* scale, int
     if (tmp) (void)hipFree(tmp);
     if (tmp_scale) (void)hipFree(tmp_scale);
     if (e != hipSuccess) {
+        (void)hipGetLastError();          // reported here, not by the next launch
         amusd_q8_matrix_free(m);
         return report(AMUSD_E_HIP, "q8_matrix", hipGetErrorString(e));
     }
@@ -705,7 +706,7 @@ int amusd_q8_cache_create(int32_t n_layers, int32_t n_seqs, int32_t n_q_heads, i
                           void* hip_stream, amusd_q8_cache** out) {
     if (!out) return report(AMUSD_E_ARG, "q8_cache: null argument");
     if (n_layers < 1 || n_seqs < 1 || n_seqs > AMUSD_MAX_SEQS || n_q_heads < 1 || n_kv_heads < 1 || n_kv_heads > 65535 || capacity < 1 ||
-        capacity > (1 << 30))
+        capacity > (1 << 24))
         return report(AMUSD_E_ARG, "q8_cache: bad sizes");
     if (head_dim != 64 && head_dim != 128) return report(AMUSD_E_ARG, "q8_cache: head_dim must be 64 or 128");
     if (block != 1 && block != 16 && block != 32 && block != 64) return report(AMUSD_E_ARG, "q8_cache: block must be 1, 16, 32 or 64");
@@ -717,6 +718,7 @@ int amusd_q8_cache_create(int32_t n_layers, int32_t n_seqs, int32_t n_q_heads, i
     hipError_t e = q8_cache_take(*c, n_layers, n_seqs, n_q_heads, n_kv_heads, head_dim, capacity, block, q8_malloc, stream);
     if (e == hipSuccess) e = hipStreamSynchronize(stream);
     if (e != hipSuccess) {
+        (void)hipGetLastError();
         amusd_q8_cache_free(c);
         return report(AMUSD_E_HIP, "q8_cache", hipGetErrorString(e));
     }
@@ -762,6 +764,7 @@ int amusd_q8_attention(amusd_q8_cache* c, int32_t layer, int32_t n_seq, const in
     const int64_t width = (int64_t)c->Hq * c->hd;
     if (!q || !out || ldq < width || ldo < width || !aligned(q, 2) || !aligned(out, 2)) return report(AMUSD_E_ARG, "q8_attention: bad rows");
     if (!(scale > 0.f) || !(scale < INFINITY)) return report(AMUSD_E_ARG, "q8_attention: scale must be positive and finite");
+    if ((int64_t)S.rows * c->G > 1 << 19) return report(AMUSD_E_ARG, "q8_attention: too many rows");      // a grid's second side ends at 65535
     Q8_TRY(launch_q8_attention(*c, layer, S, q, ldq, scale, rope_cos, rope_sin, out, ldo, static_cast<hipStream_t>(hip_stream)));
     return AMUSD_OK;
 }

@@ -396,6 +396,8 @@ static void gemm(const amusd_q8_matrix& w, const int8_t* x, int64_t ldx, const f
     }
 }
 
+constexpr int64_t kMaxLd = 1 << 22;      // the forms for many rows have 32-bit offsets into a tile's rows
+
 static int64_t work_of(const amusd_q8_matrix& w, int rows, const Q8Plan& p) {
     if (p.ways == 1) return 0;
     const int mt = q8_form_rows(p.form), nt = q8_form_tiles(p.form);
@@ -414,6 +416,7 @@ hipError_t launch_q8_gemm(const amusd_q8_matrix& w, const int8_t* x, int64_t ldx
                           void* work, int64_t work_bytes, hipStream_t stream) {
     Q8Plan plan = q8_gemm_plan(w.tiles, w.kblocks, w.gated, rows, w.cus, true);
     if (work_of(w, rows, plan) > work_bytes) plan = q8_gemm_plan(w.tiles, w.kblocks, w.gated, rows, w.cus, false);
+    if (ldx > kMaxLd) plan = {kQ8Few4x4, 1};
     auto go = [&](auto* o) {
         if (w.gated) gemm<std::remove_pointer_t<decltype(o)>, true>(w, x, ldx, scale, rows, o, ldo, plan, static_cast<int*>(work), stream);
         else gemm<std::remove_pointer_t<decltype(o)>, false>(w, x, ldx, scale, rows, o, ldo, plan, static_cast<int*>(work), stream);

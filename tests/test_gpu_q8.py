@@ -188,7 +188,7 @@ def test_gemm(gpu, rows, n, k):
     want = O.gemm(x, sx, w, sw)
     got = _np(_product(gpu, m, x, sx, n, torch.float32, ldo=n + 3))
     assert (np.abs(got - want) <= 3.01 * U32 * np.abs(want)).all()            # an exact sum, rounded, times two scales
-    half = _np(_product(gpu, m, x, sx, n, torch.bfloat16, work=False, ldx=_up16(k) + 16))
+    half = _np(_product(gpu, m, x, sx, n, torch.bfloat16, ldo=n + 1, work=False, ldx=_up16(k) + 16))
     assert np.array_equal(half, O.bf16(got).astype(np.float32))               # the same bits without a workspace, rounded once more
 
 
@@ -693,3 +693,112 @@ def test_in_a_graph(gpu):
         torch.cuda.synchronize()
         for (g, t), want in zip(graphs, wants):
             assert torch.equal(t["out"], want)
+
+
+# ---------------------------------------------------------------- far apart, side by side, refused
+def test_gemm_rows_far_apart(gpu):
+    torch, A = gpu
+    rows, n, k = 300, 512, 200
+    w, sw, m = _matrix(gpu, n, k)
+    rng = np.random.default_rng(5)
+    x, sx = rng.integers(-127, 128, (rows, k)).astype(np.int8), rng.random(rows).astype(np.float32)
+    want = _product(gpu, m, x, sx, n, torch.float32)
+    for ld in (1 << 22, (1 << 24) + 16):               # row 255 of a tile at 2^30 and past 2^32
+        xd = torch.empty((rows - 1) * ld + 256, dtype=torch.int8, device="cuda")
+        xd.as_strided((rows, k), (ld, 1)).copy_(torch.from_numpy(x))
+        s, out = torch.from_numpy(sx).cuda(), torch.empty(rows, n, dtype=torch.float32, device="cuda")
+        A.q8_gemm(m, xd.data_ptr(), ld, s.data_ptr(), rows, out.data_ptr(), A.DTYPE_FP32, n)
+        assert torch.equal(out, want), ld
+
+
+def test_products_side_by_side(gpu):
+    """Two streams, one matrix, a workspace each."""
+    torch, A = gpu
+    rows, n, k = 200, 1024, 8192
+    w, sw, m = _matrix(gpu, n, k)
+    rng = np.random.default_rng(6)
+    jobs = []
+    for i in range(2):
+        x, sx = rng.integers(-127, 128, (rows, k)).astype(np.int8), rng.random(rows).astype(np.float32)
+        want = _product(gpu, m, x, sx, n, torch.float32, work=False)
+        jobs.append((torch.from_numpy(x).cuda(), torch.from_numpy(sx).cuda(), torch.zeros(m.workspace_bytes(rows), dtype=torch.uint8, device="cuda"),
+                     torch.zeros(20, rows, n, dtype=torch.float32, device="cuda"), torch.cuda.Stream(), want))
+    torch.cuda.synchronize()
+    for r in range(20):
+        for x, s, space, out, stream, _ in jobs:
+            A.q8_gemm(m, x.data_ptr(), k, s.data_ptr(), rows, out[r].data_ptr(), A.DTYPE_FP32, n, space.data_ptr(), space.numel(), stream.cuda_stream)
+    torch.cuda.synchronize()
+    for *_, out, _, want in jobs:
+        assert (out == want).all().item()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_a_cache_past_32_bits(gpu, hd):
+    """The last sequences of a large cache hold and give what the first ones do."""
+    torch, A = gpu
+    seqs, cap, heads = (1 << 33) // (8 * (1 << 16) * hd) + 2, 1 << 16, (16, 8, hd)
+    cache = A.Q8Cache(n_layers=1, n_seqs=seqs, n_q_heads=16, n_kv_heads=8, head_dim=hd, capacity=cap, block=16)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    n, base = 70, cap - 400
+    k, v = (torch.randn(n, 8 * hd, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(n, 16, hd, generator=gen, device="cuda").to(torch.bfloat16)
+    got = []
+    for s in (0, seqs - 1):
+        for pos in (0, base):                           # an early stretch and a late one; what lies between are zeros
+            cache.append(0, [s], [pos], [n], k.data_ptr(), v.data_ptr(), 8 * hd)
+        kk, vv = (torch.empty(n, 8 * hd, dtype=torch.float32, device="cuda") for _ in range(2))
+        cache.read(0, [s], [base], [n], kk.data_ptr(), vv.data_ptr(), A.DTYPE_FP32, 8 * hd)
+        got.append((kk, vv, _attend(gpu, cache, [s], [base], [q], hd ** -0.5)[0], _attend(gpu, cache, [s], [base + n - 1], [q[:1]], hd ** -0.5)[0]))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert (got[1][0].view(n, -1) - k.float()).abs().max().item() <= k.float().abs().max().item() / 127 * 0.501
+    assert got[1][2].float().abs().max().item() > 0
+
+
+def test_refusals_with_handles(gpu):
+    torch, A = gpu
+    E = A.AmusdError
+    w, sw, m = _matrix(gpu, 8, 64)
+    x, s, out = (torch.zeros(4, 64, dtype=torch.int8, device="cuda"), torch.ones(4, device="cuda"), torch.full((4, 8), 3.0, device="cuda"))
+    good = dict(w=m, x=x.data_ptr(), ldx=64, scale=s.data_ptr(), rows=4, out=out.data_ptr(), dtype=A.DTYPE_FP32, ldo=8, workspace=0, workspace_bytes=0)
+    for bad in (dict(x=0), dict(x=x.data_ptr() + 8), dict(ldx=48), dict(ldx=72), dict(scale=0), dict(rows=-1), dict(out=0), dict(out=out.data_ptr() + 2), dict(dtype=2),
+                dict(ldo=7), dict(workspace=x.data_ptr() + 4, workspace_bytes=64), dict(workspace=x.data_ptr(), workspace_bytes=-1)):
+        with pytest.raises(E):
+            A.q8_gemm(*{**good, **bad}.values())
+    A.q8_gemm(*{**good, "rows": 0}.values())
+    with pytest.raises(E):
+        m.workspace_bytes(-1)
+    c = A.Q8Cache(n_layers=2, n_seqs=3, n_q_heads=8, n_kv_heads=2, head_dim=64, capacity=100, block=16)              # room for 128: whole tiles of 64
+    kv, q, o = (torch.zeros(4, d, dtype=torch.bfloat16, device="cuda") for d in (128, 512, 512))
+    o += 3
+    f = torch.full((4, 128), 3.0, device="cuda")
+    for layer, seqs, pos, n in ((2, [0], [0], [1]), (-1, [0], [0], [1]), (0, [3], [0], [1]), (0, [-1], [0], [1]), (0, [0, 0], [0, 1], [1, 1]), (0, [0], [-1], [2]),
+                                (0, [0], [127], [2]), (0, [0], [2 ** 31 - 1], [4]), (0, [0], [0], [0]), (0, [], [], []), (0, list(range(17)), [0] * 17, [1] * 17)):
+        with pytest.raises(E):
+            c.append(layer, seqs, pos, n, kv.data_ptr(), kv.data_ptr(), 128)
+        with pytest.raises(E):
+            c.read(layer, seqs, pos, n, f.data_ptr(), f.data_ptr(), A.DTYPE_FP32, 128)
+        with pytest.raises(E):
+            c.attention(layer, seqs, pos, n, q.data_ptr(), 512, 0.125, 0, 0, o.data_ptr(), 512)
+    one = (0, [0], [0], [1])
+    for bad in ((0, kv.data_ptr(), 128), (kv.data_ptr(), 0, 128), (kv.data_ptr(), kv.data_ptr(), 127), (kv.data_ptr() + 1, kv.data_ptr(), 128)):
+        with pytest.raises(E):
+            c.append(*one, *bad)
+    with pytest.raises(E):
+        c.append(*one, kv.data_ptr(), kv.data_ptr(), 128, f.data_ptr(), 0)
+    for bad in ((f.data_ptr(), 0, 0, 128), (f.data_ptr(), f.data_ptr(), 2, 128), (f.data_ptr() + 2, f.data_ptr(), 0, 128), (f.data_ptr(), f.data_ptr(), 0, 100)):
+        with pytest.raises(E):
+            c.read(*one, *bad)
+    for bad in ((0, 512, 0.125, 0, 0, o.data_ptr(), 512), (q.data_ptr(), 511, 0.125, 0, 0, o.data_ptr(), 512), (q.data_ptr(), 512, 0.0, 0, 0, o.data_ptr(), 512),
+                (q.data_ptr(), 512, float("inf"), 0, 0, o.data_ptr(), 512), (q.data_ptr(), 512, float("nan"), 0, 0, o.data_ptr(), 512),
+                (q.data_ptr(), 512, 0.125, f.data_ptr(), 0, o.data_ptr(), 512), (q.data_ptr(), 512, 0.125, 0, 0, o.data_ptr(), 500)):
+        with pytest.raises(E):
+            c.attention(*one, *bad)
+    with pytest.raises(E):
+        A.Q8Cache(n_layers=64, n_seqs=64, n_q_heads=8, n_kv_heads=8, head_dim=128, capacity=1 << 24, block=64)       # more memory than there is; nothing is left behind for the next call
+    long = A.Q8Cache(n_layers=1, n_seqs=1, n_q_heads=8, n_kv_heads=1, head_dim=64, capacity=1 << 17, block=64)
+    with pytest.raises(E):
+        long.attention(0, [0], [0], [(1 << 16) + 1], q.data_ptr(), 512, 0.125, 0, 0, o.data_ptr(), 512)
+    c.append(*one, kv.data_ptr(), kv.data_ptr(), 128)
+    torch.cuda.synchronize()
+    assert (out == 3).all().item() and (o == 3).all().item() and (f == 3).all().item()

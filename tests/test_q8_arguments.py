@@ -55,7 +55,7 @@ def test_matrix_and_product(L):
 def test_cache(L):
     good = dict(n_layers=1, n_seqs=1, n_q_heads=8, n_kv_heads=2, head_dim=64, capacity=64, block=1, stream=NULL)
     h = C.c_void_p()
-    for change in (dict(n_layers=0), dict(n_seqs=0), dict(n_seqs=5000), dict(n_q_heads=6), dict(n_kv_heads=0), dict(n_q_heads=32), dict(head_dim=96), dict(capacity=0),
+    for change in (dict(n_layers=0), dict(n_seqs=0), dict(n_seqs=5000), dict(n_q_heads=6), dict(n_kv_heads=0), dict(n_q_heads=32), dict(head_dim=96), dict(capacity=0), dict(capacity=(1 << 24) + 1),
                    dict(block=0), dict(block=8), dict(block=128)):
         _refused(L.amusd_q8_cache_create(*{**good, **change}.values(), C.byref(h)), L)
         assert not h

@@ -309,8 +309,8 @@ __global__ void __launch_bounds__(256) k_q8_append(amusd_q8_cache C, int layer, 
         ratio[t] = r;
     }
     __syncthreads();
-    // Keys: 16 columns of a position a thread; values: 4 positions of columns c and c + 16 (kept as q + 128: amusd_q8_attention.hip).  What a block that this call reaches held before is rounded again where its
-    // scale has grown.
+    // Keys: 16 columns of a position a thread; values: 4 positions of columns c and c + 16 (kept as q + 128: amusd_q8_attention.hip).
+    // What a block that this call reaches held before is rounded again where its scale has grown.
     int8_t* out = (values ? C.v : C.k) + kvh * ((size_t)C.cap * HD);
     const int first_row = max(0, (from & -B) - p0), last_row = to - p0;           // rows that can change
     auto fresh = [&](int r) { return p0 + r >= from && p0 + r < to; };
@@ -367,6 +367,7 @@ __global__ void __launch_bounds__(256) k_q8_append(amusd_q8_cache C, int layer, 
             }
         }
     }
+    wait_vm<0>();          // a wave does not end with loads under way
 }
 
 hipError_t launch_q8_append(const amusd_q8_cache& c, int layer, const Q8Segs& S, const void* k, const void* v, int64_t ld, const float* cos,
@@ -412,6 +413,7 @@ __global__ void __launch_bounds__(256) k_q8_read(amusd_q8_cache C, int layer, Q8
             __builtin_memcpy(out + (int64_t)pos * ld + x * 4, v, sizeof v);
         }
     }
+    wait_vm<0>();
 }
 
 hipError_t launch_q8_read(const amusd_q8_cache& c, int layer, const Q8Segs& segs, void* k, void* v, int dtype, int64_t ld, hipStream_t stream) {

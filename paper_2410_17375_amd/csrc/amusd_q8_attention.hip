@@ -394,6 +394,7 @@ __global__ void __launch_bounds__(64, HD == 64 ? 3 : 1) k_q8_att_part(amusd_q8_c
             out[(HD + 1) * 16 + pair] = sums.den;
         }
     });
+    wait_vm<0>();          // a wave does not end with loads under way
 }
 
 __device__ __forceinline__ uint16_t q8_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
@@ -460,6 +461,7 @@ __global__ void __launch_bounds__(HD * 2) k_q8_att_merge(amusd_q8_cache C, Q8Seg
         }
         if (c0 + kRound < most) __syncthreads();
     }
+    wait_vm<0>();
     if (pair >= pairs) return;
     const int row = (first + pair) / C.G, head = kvh * C.G + (first + pair) % C.G;
     Q.out[(int64_t)(seg.row0 + row) * Q.ldo + (int64_t)head * HD + col] = q8_bf16(acc / den);
@@ -491,6 +493,7 @@ __global__ void __launch_bounds__(64, HD == 64 ? 3 : 2) k_q8_att_whole(amusd_q8_
             all[d][lane] = v;
         }
     });
+    wait_vm<0>();
     if (T.pos < 0) return;
     const int pair = W.local * 16 + (lane & 15);
     uint16_t* out = Q.out + (int64_t)(W.seg->row0 + pair / C.G) * Q.ldo + (int64_t)(kvh * C.G + pair % C.G) * HD + (lane >> 4) * 4;

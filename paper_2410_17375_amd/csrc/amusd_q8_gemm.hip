@@ -74,10 +74,9 @@ __global__ void __launch_bounds__(512) k_q8_gemm_rows(const uint4* __restrict__ 
             }
         }
 #pragma unroll
-        for (int d = 0; d < D; ++d) {
-            asm volatile("" ::"v"(wf[d][0].x), "v"(xf[d][0].x));     // a wave does not end with loads under way
+        for (int d = 0; d < D; ++d)
             if (i + d < S) use(d);
-        }
+        wait_vm<0>();          // a wave does not end with loads under way
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m)

@@ -56,7 +56,8 @@ extern "C" {
 #define AMUSD_DTYPE_INT8    2   /* an 8-bit model: tensors come in bf16 as with AMUSD_DTYPE_BF16, matrices and cache are held as signed 8 bits with
                                   * fp32 scales (a feature, a position and kv head), embedding and gains as they are.  A pass is the 8-bit operators
                                   * below one after the other.  It is another model than the bf16 one of the same tensors, and keeps
-                                  * the same promises: exact loops, rows whose bits depend on their sequence alone */
+                                  * the same promises: exact loops, rows whose bits depend on their sequence alone.  Widths are at
+                                  * most 131072, max_ctx 2^24 (else ARG) */
 #define AMUSD_MAX_K        16   /* rows of one pass: the 16-row matrix-core tile */
 #define AMUSD_MAX_SEQS   4096   /* sequences (key-value caches) one model can hold */
 

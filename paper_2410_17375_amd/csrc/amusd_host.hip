@@ -211,6 +211,8 @@ int check_config(const amusd_config* c) {
     const long qdim = (long)c->n_q_heads * c->head_dim;
     if (c->d_model % kb || qdim % kb || c->d_ffn % kb)
         return fail(AMUSD_E_ARG, "config: d_model, n_q_heads*head_dim and d_ffn must be multiples of the fragment width");
+    if (c->dtype == AMUSD_DTYPE_INT8 && (c->d_model > kQ8MaxK || qdim > kQ8MaxK || c->d_ffn > kQ8MaxK || c->max_ctx > kQ8MaxPositions))
+        return fail(AMUSD_E_ARG, "config: an 8-bit model's widths are at most 131072, its context 2^24");
     if (c->d_model % 16 || c->d_ffn % 16 || c->vocab % 16)
         return fail(AMUSD_E_ARG, "config: d_model, d_ffn and vocab must be multiples of 16");
     if (!(c->rope_theta > 0.f) || !(c->rms_eps >= 0.f)) return fail(AMUSD_E_ARG, "config: rope_theta/rms_eps");
@@ -500,7 +502,7 @@ int take_prefill(amusd_model* m) {
     if (e == hipSuccess) e = hipHostGetDevicePointer(&host_dev, m->pf_host, 0);
     if (e == hipSuccess) {
         layout(reinterpret_cast<uintptr_t>(m->pf_mem));
-        if (m->q8) {                               // (products leave their workspace as they find it: zeros)
+        if (m->q8) {                               // products take a workspace that was zeroed once
             e = m->q8_pf.work_bytes ? launch_fill_zero(static_cast<uint4*>(m->q8_pf.work), (size_t)m->q8_pf.work_bytes / 16, m->stream) : hipSuccess;
             if (e == hipSuccess) e = hipStreamSynchronize(m->stream);
         } else e = hipMemcpy(dev_orders, orders.data(), orders.size() * 4, hipMemcpyHostToDevice);
@@ -1207,12 +1209,17 @@ int amusd_seq_get_kv(amusd_model* m, int32_t seq, int32_t layer, int32_t which, 
     int rc = need_ready(m);
     if (rc || (rc = need_seq(m, seq))) return rc;
     const DevModel& D = m->dm;
-    if (!out || layer < 0 || layer >= D.n_layers || (which != 0 && which != 1) || pos0 < 0 || n < 1 || pos0 + n > D.ctx_pad)
+    if (!out || layer < 0 || layer >= D.n_layers || (which != 0 && which != 1) || pos0 < 0 || n < 1 || (int64_t)pos0 + n > D.ctx_pad)
         return fail(AMUSD_E_ARG, "get_kv: bad argument");
     if (m->q8) {
         const size_t width = (size_t)D.Hkv * D.hd;
         if (pos0 + n > D.max_ctx) return fail(AMUSD_E_ARG, "get_kv: bad argument");
-        std::vector<float> rows((size_t)n * width);
+        std::vector<float> rows;
+        try {
+            rows.resize((size_t)n * width);
+        } catch (const std::bad_alloc&) {
+            return fail(AMUSD_E_NOMEM, "get_kv: rows");
+        }
         void* dev = nullptr;
         HIP_TRY(dev_malloc(m->device, &dev, 2 * rows.size() * 4));
         float* const kv = static_cast<float*>(dev);

@@ -711,7 +711,7 @@ int amusd_q8_cache_create(int32_t n_layers, int32_t n_seqs, int32_t n_q_heads, i
                           void* hip_stream, amusd_q8_cache** out) {
     if (!out) return report(AMUSD_E_ARG, "q8_cache: null argument");
     if (n_layers < 1 || n_seqs < 1 || n_seqs > AMUSD_MAX_SEQS || n_q_heads < 1 || n_kv_heads < 1 || n_kv_heads > 65535 || capacity < 1 ||
-        capacity > (1 << 24))
+        capacity > kQ8MaxPositions)
         return report(AMUSD_E_ARG, "q8_cache: bad sizes");
     if (head_dim != 64 && head_dim != 128) return report(AMUSD_E_ARG, "q8_cache: head_dim must be 64 or 128");
     if (block != 1 && block != 16 && block != 32 && block != 64) return report(AMUSD_E_ARG, "q8_cache: block must be 1, 16, 32 or 64");

@@ -170,6 +170,7 @@ int q8_model_create(const DevModel& D, int, Q8Alloc alloc, hipStream_t stream, Q
     // extended again is the cache that was extended once.
     if (e == hipSuccess) e = q8_cache_take(q->cache, D.n_layers, D.n_slots, D.Hq, D.Hkv, D.hd, D.max_ctx, 1, alloc, stream);
     if (e != hipSuccess) {
+        (void)hipGetLastError();          // reported here, not by the next launch
         q8_model_free(q);
         return report(AMUSD_E_HIP, "8-bit model", hipGetErrorString(e));
     }

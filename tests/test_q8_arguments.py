@@ -67,6 +67,17 @@ def test_cache(L):
     assert L.amusd_q8_attention(None, 0, 1, one, one, one, P, 512, 0.125, None, None, P, 512, None) == -1
 
 
+def test_models(L):
+    import paper_2410_17375_amd as A
+    good = dict(n_layers=1, d_model=64, n_q_heads=1, n_kv_heads=1, head_dim=64, d_ffn=64, vocab=64, max_ctx=64, max_k=8, dtype=A.DTYPE_INT8, rope_theta=1e4,
+                rms_eps=1e-5, max_seqs=1)
+    h = C.c_void_p()
+    for change in (dict(d_ffn=131072 + 64), dict(d_model=131072 + 64), dict(max_ctx=(1 << 24) + 1), dict(dtype=3), dict(d_ffn=48)):
+        cfg = A.Config(*{**good, **change}.values())
+        _refused(L.amusd_model_create(C.byref(cfg), None, C.byref(h)), L)
+        assert not h
+
+
 def test_calls_need_a_device(L):
     torch = pytest.importorskip("torch")
     if torch.cuda.is_available():

@@ -18,7 +18,7 @@ namespace amusd {
 // element are in 64 bits, the element then rounded to 32: a square of a large element stays finite.
 // The quotient is taken as the product with the scale's reciprocal, and divided in full only where that is too near the middle between
 // two integers to tell (half the largest value stands on one); adding 1.5 * 2^23 leaves the nearest integer, ties to even, in the low bits.
-// Measured (MI355X): 2048 x 14336 bf16 28 us (3.2 TB/s; a division for each element 53), 2048 x 4096 fp32 + bf16 with norm and sum 24 (3.8 TB/s),
+// Measured (MI355X): 2048 x 14336 bf16 23-26 us (3.4-3.9 TB/s; a division for each element 53), 2048 x 4096 fp32 + bf16 with norm and sum 25 (3.7 TB/s),
 // 1531 x 2055 14.5 (rows of odd length), 8 x 4096 with norm 5.7, 1 x 2048 2.5.
 template <class T>
 __device__ __forceinline__ void q8_load(const T* p, int n, float (&v)[8]) {       // n: elements there are, 1 or more
@@ -202,15 +202,18 @@ __global__ void __launch_bounds__(1024) k_q8_rows(const X* x, int64_t ldx, const
 template <class X, class A, bool NORM>
 static void q8_rows(const void* x, int64_t ldx, const void* add, int64_t ldadd, const float* gain, float eps, int rows, int n, void* sum, int64_t ldsum,
                     int8_t* q, int64_t ldq, float* scale, hipStream_t stream) {
-    // two vectors of 8 a thread; one where the rows are so few that only the way through one counts
-    const int per = rows <= 128 && n <= 8 * 1024 ? 8 : 16;
-    const int threads = std::min(1024, std::max(64, (n + per * 64 - 1) / (per * 64) * 64));
+    // Vectors of 8 elements a thread, where only the largest is sought: one for few rows, as then the way through one row counts (8 x 14336 5.8 us for
+    // 6.2); four for many and long ones, for more workgroups a compute unit, in different phases (2048 x 14336 22.8 us for 25.4; 2048 x 4096 and
+    // x 8192 10.4 for 9.4 and 15.9 for 15.3).  A norm has two whatever the number of rows: its sum of squares has its order from that.
+    const int vectors = NORM ? 2 : rows <= 128 ? 1 : rows > 1024 && n > 8 * 1024 ? 4 : 2;
+    const int threads = std::min(1024, std::max(64, (n + vectors * 512 - 1) / (vectors * 512) * 64));
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3(rows), dim3(threads), 0, stream, static_cast<const X*>(x), ldx, static_cast<const A*>(add), ldadd, gain, eps, n,
                            static_cast<X*>(sum), ldsum, q, ldq, scale);
     };
     if (n <= 8 * threads) launch(k_q8_rows<X, A, NORM, 1>);
     else if (n <= 2 * 8 * threads) launch(k_q8_rows<X, A, NORM, 2>);
+    else if (!NORM && n <= 4 * 8 * threads) launch(k_q8_rows<X, A, NORM, NORM ? 2 : 4>);
     else launch(k_q8_rows<X, A, NORM, 0>);
 }
 

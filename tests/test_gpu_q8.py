@@ -77,6 +77,22 @@ def test_quantize(gpu, rows, n, dtype):
     assert (got[:, n:] == 99).all()
 
 
+@pytest.mark.parametrize("n", [8200, 14336, 20001])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_quantize_many_rows_as_few(gpu, n, dtype):
+    """Rows are laid over threads otherwise where they are many and long."""
+    torch, A = gpu
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.randn(1100, n, generator=gen, device="cuda").to(getattr(torch, dtype))
+    got = []
+    for step in (1100, 100):
+        q, s = torch.zeros((1100, _up16(n)), dtype=torch.int8, device="cuda"), torch.empty(1100, device="cuda")
+        for r in range(0, 1100, step):
+            A.q8_quantize(x[r].data_ptr(), _code(A, torch, x), n, step, n, q[r].data_ptr(), q.shape[1], s[r:].data_ptr())
+        got.append((q, s))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
 def test_quantize_special_rows(gpu):
     torch, A = gpu
     n = 50
@@ -121,6 +137,24 @@ def test_rmsnorm(gpu, rows, n, dtype, add, inplace):
     assert np.array_equal(_np(out), torch.from_numpy(want_sum).to(kind[dtype]).float().numpy())
     # sums of n squares and a root in 64 bits: n + 4 roundings of 2^-53; eps is a float32
     _check_q8(_np(q)[:, :n].astype(np.int64), _np(s), O.rmsnorm(want_sum, None, _np(gain), float(np.float32(1e-5)))[1], (n + 8) * 2.0 ** -53)
+
+
+@pytest.mark.parametrize("n", [512, 1030, 2048, 4096, 5120, 14336, 16384])
+def test_rmsnorm_rows_keep_their_bits(gpu, n):
+    torch, A = gpu
+    rows = 1500
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    x, gain = torch.randn(rows, n, generator=gen, device="cuda"), torch.rand(n, generator=gen, device="cuda") + 0.5
+
+    def norm(first, count):
+        q, s = torch.zeros((count, _up16(n)), dtype=torch.int8, device="cuda"), torch.empty(count, device="cuda")
+        A.q8_rmsnorm(x[first].data_ptr(), 0, n, 0, 0, 0, gain.data_ptr(), 1e-5, count, n, 0, 0, q.data_ptr(), q.shape[1], s.data_ptr())
+        return q, s
+
+    q, s = norm(0, rows)
+    for first, count in ((0, 1), (1, 8), (9, 128), (137, 129), (266, 1024), (1290, 210)):
+        a, b = norm(first, count)
+        assert torch.equal(a, q[first:first + count]) and torch.equal(b, s[first:first + count])
 
 
 def test_rmsnorm_of_huge_and_of_nonfinite_rows(gpu):

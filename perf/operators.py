@@ -181,6 +181,7 @@ def prepare(case, seed):
     s = {"op": op, **{k: v for k, v in case.items() if k != "name"}}
     if op in ("quantize", "rmsnorm"):
         rows, n = case["rows"], case["n"]
+        s.pop("add")                                              # (the case's: a type, or that there is none)
         s.update(t)
         s["q8"] = torch.zeros(rows, _pad16(n), dtype=torch.int8, device="cuda")
         s["scale"] = torch.empty(rows, device="cuda")

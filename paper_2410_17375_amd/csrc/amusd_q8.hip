@@ -94,7 +94,8 @@ __device__ __forceinline__ void q8_round(const float (&v)[N], float s, float inv
         far = fmaxf(far, fabsf(t - (r - 12582912.f)));
         b[i] = inv > 0.f ? __float_as_uint(r) : 0u;
     }
-    if (far > 0.49998f && inv > 0.f)             // (t is off by at most 127 * 2^-23)
+    // (t is off by at most 127 * 2^-23.  A scale below 2^-128 has no finite reciprocal: t then says nothing.)
+    if ((far > 0.49998f || inv > 3.4028235e38f) && inv > 0.f)
 #pragma unroll
         for (int i = 0; i < N; ++i) b[i] = (uint32_t)(int)rintf(v[i] / s);
 }

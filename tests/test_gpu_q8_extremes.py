@@ -1,0 +1,71 @@
+"""The 8-bit operators at the ends of the number range: scales that are subnormal, values and keys near the largest float32, queries near
+the smallest.  Tolerances are counted in roundings as in test_gpu_q8.py."""
+import numpy as np
+import pytest
+
+from oracle import q8 as O
+from test_gpu_q8 import U16, U32, _append, _attend, _check_q8, _np, _product, _rand, _read, _strided, _tolerance, gpu  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _rows_of(rng, most, n):
+    """A row for each magnitude: random values up to it, and the magnitude itself."""
+    a = rng.uniform(-1, 1, (len(most), n))
+    a[:, ::7] *= 2.0 ** -5
+    a[:, n // 2] = np.where(np.arange(len(most)) % 2, -1, 1)
+    return (a * np.asarray(most, dtype=np.float64)[:, None]).astype(np.float32)
+
+
+# magnitudes around those whose scale (a 127th) has no finite reciprocal in float32 (below 3.7e-37), and around subnormal ones
+SMALL = [4e-37, 3.8e-37, 3.6e-37, 3e-37, 1e-37, 1.2e-38, 1e-38, 3e-39, 1e-40, 3e-41]
+
+
+# ---------------------------------------------------------------- scales without a reciprocal
+@pytest.mark.parametrize("n", [50, 2055, 20001])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_quantize_small_rows(gpu, n, dtype):
+    torch, A = gpu
+    x = torch.from_numpy(_rows_of(np.random.default_rng(n), SMALL, n)).to(getattr(torch, dtype)).cuda()
+    ld = -(-n // 16) * 16
+    q, s = torch.empty((len(SMALL), ld), dtype=torch.int8, device="cuda"), torch.empty(len(SMALL), device="cuda")
+    A.q8_quantize(x.data_ptr(), A.DTYPE_FP32 if dtype == "float32" else A.DTYPE_BF16, n, len(SMALL), n, q.data_ptr(), ld, s.data_ptr())
+    want, scale, _ = O.quantize(_np(x))
+    assert np.array_equal(_np(s), scale)
+    assert np.array_equal(_np(q)[:, :n], want)
+    live = _np(x).any(1)                                  # (3e-41 is below half of bf16's smallest: a row of zeros)
+    assert live[:-1].all() and (np.abs(_np(q)[live, :n]).max(1) == 127).all()
+
+
+@pytest.mark.parametrize("n", [96, 1030, 17000])
+def test_rmsnorm_small_gains(gpu, n):
+    torch, A = gpu
+    rng = np.random.default_rng(n)
+    x = torch.from_numpy(rng.standard_normal((3, n)).astype(np.float32)).cuda()
+    for size in (2e-37, 1e-38):
+        gain = torch.from_numpy(((1 + 0.1 * rng.standard_normal(n)) * size / 4).astype(np.float32)).cuda()
+        ld = -(-n // 16) * 16
+        q, s = torch.empty((3, ld), dtype=torch.int8, device="cuda"), torch.empty(3, device="cuda")
+        A.q8_rmsnorm(x.data_ptr(), 0, n, 0, 0, 0, gain.data_ptr(), 1e-5, 3, n, 0, 0, q.data_ptr(), ld, s.data_ptr())
+        y = O.rmsnorm(_np(x), None, _np(gain), float(np.float32(1e-5)))[1]
+        _check_q8(_np(q)[:, :n].astype(np.int64), _np(s), y, (n + 8) * 2.0 ** -53)
+        assert (np.abs(_np(q)[:, :n]).max(1) == 127).all()
+
+
+@pytest.mark.parametrize("block", [1, 32])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_append_small_rows(gpu, block, hd):
+    """Pieces that grow from magnitudes whose scale has no reciprocal; blocks that hold them are rounded again."""
+    torch, A = gpu
+    cache = A.Q8Cache(n_layers=1, n_seqs=1, n_q_heads=2, n_kv_heads=2, head_dim=hd, capacity=256, block=block)
+    ref = [O.Cache(2, hd, 256, block) for _ in range(2)]
+    rng, at = np.random.default_rng(hd), 0
+    for n, size in ((5, 1e-39), (9, 5e-38), (40, 1e-37), (30, 3e-37), (64, 2e-37), (3, 1e-36), (20, 1.0)):
+        k, v = (torch.from_numpy(_rows_of(rng, [size] * (n * 2), hd).reshape(n, 2, hd)).to(torch.bfloat16).cuda() for _ in range(2))
+        _append(gpu, cache, [0], [at], [k], [v])
+        ref[0].append(at, _np(k))
+        ref[1].append(at, _np(v))
+        at += n
+    for got, want in zip(_read(gpu, cache, 0, 0, at, 2, hd), ref):
+        assert np.array_equal(got, want.values(at).astype(np.float32))
+        assert got[:5].any() and got[54:84].any()

@@ -283,7 +283,8 @@ int amusd_generate_greedy(amusd_model *m, const int32_t *prompt, int32_t n_promp
  * product of such rows with an 8-bit matrix, and attention over a cache in 8 bits.
  *
  * 8 bits stand for x ~ q * s, q an integer in [-127, 127]: s = max|x| / 127 over the values that share the scale, q the quotient
- * x / s (both in float32) rounded to the nearest integer, ties to even.  s = 0 where all values are 0.  Values that are not finite give
+ * x / s (both in float32) rounded to the nearest integer, ties to even, and to +-127 where a scale of a few units of
+ * the smallest float32 lets it be more.  s = 0 where all values are 0 (or too small for a scale: below 9e-44).  Values that are not finite give
  * s = NaN and q = 0, so that what is computed from them is NaN too.
  *
  * All pointers are device memory of the current device unless said otherwise, but arrays of sequence ids, positions and

@@ -84,6 +84,8 @@ __device__ __forceinline__ float q8_scale(uint32_t bits, float& inv) {
     inv = s > 0.f ? (float)(1. / (double)s) : 0.f;
     return s;
 }
+// The nearest integer to v / s.  A scale of a few units of the smallest number is rounded so far that the quotient can be past 127.
+__device__ __forceinline__ int q8_quotient(float v, float s) { return (int)rintf(fminf(fmaxf(v / s, -127.f), 127.f)); }
 // Low bytes: the float32 quotients v[i] / s rounded to the nearest integer (0 where there is no scale).
 template <int N>
 __device__ __forceinline__ void q8_round(const float (&v)[N], float s, float inv, uint32_t (&b)[N]) {
@@ -97,7 +99,7 @@ __device__ __forceinline__ void q8_round(const float (&v)[N], float s, float inv
     // (t is off by at most 127 * 2^-23.  A scale below 2^-128 has no finite reciprocal: t then says nothing.)
     if ((far > 0.49998f || inv > 3.4028235e38f) && inv > 0.f)
 #pragma unroll
-        for (int i = 0; i < N; ++i) b[i] = (uint32_t)(int)rintf(v[i] / s);
+        for (int i = 0; i < N; ++i) b[i] = (uint32_t)q8_quotient(v[i], s);
 }
 __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0C0C0400u), __builtin_amdgcn_perm(b, a, 0x0C0C0400u), 0x05040100u);
@@ -467,7 +469,7 @@ __global__ void __launch_bounds__(64) k_q8_matrix(uint4* __restrict__ frag, floa
         int8_t b = 0;
         if (c < k) {
             if constexpr (sizeof(T) == 1) b = (int8_t)w[c];
-            else b = inv > 0.f ? (int8_t)(int)rintf(value(c) / s) : (int8_t)0;
+            else b = inv > 0.f ? (int8_t)q8_quotient(value(c), s) : (int8_t)0;
         }
         out[(((size_t)tile * kblocks + kb) * 64 + (lane >> 4) * 16 + r) * 16 + (lane & 15)] = b;
     }

@@ -69,3 +69,46 @@ def test_append_small_rows(gpu, block, hd):
     for got, want in zip(_read(gpu, cache, 0, 0, at, 2, hd), ref):
         assert np.array_equal(got, want.values(at).astype(np.float32))
         assert got[:5].any() and got[54:84].any()
+
+
+# ---------------------------------------------------------------- scales of a few units of the smallest number: quotients past 127
+UNIT = 2.0 ** -149
+FEW = [64 * UNIT, 100 * UNIT, 143 * UNIT, 190 * UNIT, 191 * UNIT, 260 * UNIT, 317 * UNIT, 1000 * UNIT, 3.3e-42, 2e-41]
+
+
+def test_quotients_past_127(gpu):
+    torch, A = gpu
+    n = 70
+    rows = _rows_of(np.random.default_rng(1), FEW, n)
+    assert (np.abs(rows[3] / (np.abs(rows[3]).max() / np.float32(127))) > 128).any()
+    x = torch.from_numpy(rows).cuda()
+    q, s = torch.empty((len(FEW), 80), dtype=torch.int8, device="cuda"), torch.empty(len(FEW), device="cuda")
+    A.q8_quantize(x.data_ptr(), A.DTYPE_FP32, n, len(FEW), n, q.data_ptr(), 80, s.data_ptr())
+    want, scale, _ = O.quantize(rows)
+    assert np.array_equal(_np(s), scale)
+    assert np.array_equal(_np(q)[:, :n], want)
+    # a matrix's rows, read off through unit vectors
+    for w in (rows, _rows_of(np.random.default_rng(2), SMALL, n)):
+        m = A.Q8Matrix(w, A.DTYPE_FP32, len(w), n)
+        got = _np(_product(gpu, m, np.eye(n, dtype=np.int8), np.ones(n, np.float32), len(w), torch.float32)).T
+        want, scale, _ = O.quantize(w)
+        assert np.array_equal(got, (want * scale[:, None].astype(np.float64)).astype(np.float32))
+
+
+@pytest.mark.parametrize("block", [1, 16])
+def test_quotients_past_127_in_the_cache(gpu, block):
+    """Rotary turns keys to magnitudes that bf16 itself does not have: a few units of the smallest float32."""
+    torch, A = gpu
+    hd, n = 64, 40
+    cache = A.Q8Cache(n_layers=1, n_seqs=1, n_q_heads=2, n_kv_heads=2, head_dim=hd, capacity=64, block=block)
+    rng = np.random.default_rng(5)
+    k = torch.from_numpy(_rows_of(rng, [1.0] * (n * 2), hd).reshape(n, 2, hd)).to(torch.bfloat16).cuda()
+    size = np.asarray(FEW * 4, dtype=np.float32)[:, None]
+    if block > 1:
+        size[:] = 190 * UNIT
+    cos, sin = torch.from_numpy(np.repeat(size, hd // 2, 1)).cuda(), torch.zeros((n, hd // 2), device="cuda")
+    _append(gpu, cache, [0], [0], [k], [k], rope=(cos.data_ptr(), sin.data_ptr()))
+    ref = O.Cache(2, hd, 64, block)
+    ref.append(0, _np(k) * np.repeat(size, 1, 1)[:, :, None])
+    kk, _ = _read(gpu, cache, 0, 0, n, 2, hd)
+    assert np.array_equal(kk, ref.values(n).astype(np.float32))

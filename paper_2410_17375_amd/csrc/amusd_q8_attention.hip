@@ -132,6 +132,7 @@ struct Sums {
 
 // Scales of a chunk's keys and values, 8 keys a lane: two loads of the wave have those of a longest chunk.
 constexpr int kMaxChunk = 512;
+constexpr int kWalkLds = 2 * kMaxChunk + 64;     // floats: a chunk's scales, and one of each lane's that is rarely read
 struct Scales {
     v4f k[2], v[2];
 };
@@ -190,6 +191,12 @@ __device__ __forceinline__ Values<HD> load_values(const amusd_q8_cache& C, size_
     return B;
 }
 
+// Weights are lifted by at most 2^60 with their own exponent, as 2^x has to leave small ones; where the values' scales want more (below 2^-50, or
+// from 2^71 on) the rest goes with the scale.  Numerators of such large values would be past float32 before they are divided: they are
+// kept kDown times what they are, which a denominator below 0 says.
+constexpr int kMaxLift = 60;
+constexpr float kDown = 0x1p-40f;
+
 constexpr float kSlack = 4.f;                    // a maximum may exceed its reference by 2^4 before the sums are rescaled
 
 // A step's scores, without the query's factor.
@@ -209,10 +216,10 @@ __device__ __forceinline__ void step_scores(const Keys<HD>& K, const Tile<HD>& T
     }
 }
 
-// .. and its weights, as the values' product takes them, 2^lift times what they are.  MASK: some pair does not see all of its keys.
-// left: keys from the step's first one up to the last that the lane's pair sees.
-template <int HD, bool MASK>
-__device__ __forceinline__ void step_weights(float (&sc)[4][4], float qs, const v4f* vs, float lift, int left, Sums<HD>& S, uint4 (&out)[2]) {
+// .. and its weights, as the values' product takes them, 2^lift (FAR: and post) times what they are.  MASK: some pair does not see all of
+// its keys.  left: keys from the step's first one up to the last that the lane's pair sees.
+template <int HD, bool MASK, bool FAR>
+__device__ __forceinline__ void step_weights(float (&sc)[4][4], float qs, const v4f* vs, float lift, float post, int left, Sums<HD>& S, uint4 (&out)[2]) {
     const int g4 = (threadIdx.x & 48) >> 2;
     float top[4];
 #pragma unroll
@@ -238,7 +245,8 @@ __device__ __forceinline__ void step_weights(float (&sc)[4][4], float qs, const 
     float sum[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        const v4f scale = vs[t * 4];
+        v4f scale = vs[t * 4];
+        if (FAR) scale *= post;
         float p[4], w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -254,13 +262,26 @@ __device__ __forceinline__ void step_weights(float (&sc)[4][4], float qs, const 
     S.den += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
-// sums so far and a chunk's: how both are weighed
-__device__ __forceinline__ void merge_weights(float& ref, float& den, float cref, float cden, float& a, float& b) {
+// sums so far and a chunk's: how both are weighed.  down: whether the numerators so far are kDown times what they are.
+__device__ __forceinline__ void merge_weights(float& ref, float& den, bool& down, float cref, float cden, float& a, float& b) {
     const float to = fmaxf(ref, cref), at = to == -INFINITY ? 0.f : to;
     a = pow2(ref - at);
     b = pow2(cref - at);
-    den = fmaf(den, a, cden * b);
+    den = fmaf(den, a, fabsf(cden) * b);
     ref = to;
+    if (cden < 0.f) {
+        if (!down) a *= kDown;
+        down = true;
+    } else if (down) {
+        b *= kDown;
+    }
+}
+
+// The lane, such that addresses made of it are found where they are used, once a chunk, and not kept in registers through its steps.
+__device__ __forceinline__ int lane_anew() {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
 }
 
 // Walks the keys [begin, end) (multiples of a step; begin a chunk's) and calls done(chunk's first key, its sums) at the end of each chunk.
@@ -269,14 +290,17 @@ __device__ __forceinline__ void merge_weights(float& ref, float& den, float cref
 template <int HD, bool PER_TOKEN, class Done>
 __device__ __forceinline__ void walk(const amusd_q8_cache& C, size_t kvh, const Tile<HD>& T, int least, int begin, int end, Keys<HD> K, Scales sc,
                                      float* lds, Done&& done) {
-    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const int g = (threadIdx.x & 63) >> 4;
     v4f* const kl = reinterpret_cast<v4f*>(lds);
     v4f* const vl = reinterpret_cast<v4f*>(lds + kMaxChunk);
+    auto post = [&]() -> float& { return lds[2 * kMaxChunk + lane_anew()]; };
     Sums<HD> S;
     float lift = 0.f;
-    int c0 = begin;
+    bool far = false;
+    int c0 = begin, plain = least;               // plain: the last key up to which steps are of the common kind
     auto chunk_begin = [&](int b) {
         c0 = b;
+        const int lane = lane_anew(), g = lane >> 4;
         __builtin_amdgcn_wave_barrier();
         float all = 0.f;
 #pragma unroll
@@ -302,7 +326,11 @@ __device__ __forceinline__ void walk(const amusd_q8_cache& C, size_t kvh, const 
         }
         most = fmaxf(most, lane_xor<16>(most));
         most = fmaxf(most, lane_xor<32>(most));
-        lift = (float)(10 - min(max((int)(__float_as_uint(most) >> 23) - 127, -100), 100));
+        const int all_of_it = most > 0.f ? 137 - (int)(__float_as_uint(most) >> 23) : 0, here = min(max(all_of_it, -kMaxLift), kMaxLift);
+        lift = (float)here;
+        far = __any(all_of_it != here);
+        plain = far ? -1 : least;
+        if (far) post() = __uint_as_float((uint32_t)(127 + all_of_it - here) << 23);
         S.ref = -INFINITY;
         S.den = 0.f;
         S.weights = v4f{0.f, 0.f, 0.f, 0.f};
@@ -320,8 +348,9 @@ __device__ __forceinline__ void walk(const amusd_q8_cache& C, size_t kvh, const 
         if (more) K = load_keys<HD>(C, kvh, b + kStep);
         if (ends && more) sc = load_scales<PER_TOKEN>(C, kvh, b + kStep);
         uint4 w[2];
-        if (b + kStep - 1 <= least) step_weights<HD, false>(sc4, T.qs, vs, lift, 0, S, w);
-        else step_weights<HD, true>(sc4, T.qs, vs, lift, T.pos - b, S, w);
+        if (b + kStep - 1 <= plain) step_weights<HD, false, false>(sc4, T.qs, vs, lift, 1.f, 0, S, w);
+        else if (__builtin_expect(!far, 1)) step_weights<HD, true, false>(sc4, T.qs, vs, lift, 1.f, T.pos - b, S, w);
+        else step_weights<HD, true, true>(sc4, T.qs, vs, lift, post(), T.pos - b, S, w);
         const uint4 ones{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -348,6 +377,13 @@ __device__ __forceinline__ void walk(const amusd_q8_cache& C, size_t kvh, const 
             for (int d = 0; d < HD / 16; ++d)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) S.acc[d][e] = fmaf(-1152.f, S.weights[e], S.acc[d][e]) * down;
+            if (__builtin_expect(far, 0)) {
+                const float more = post();
+                const float rest = more < 1.f ? kDown / more : 1.f / more;          // (powers of two)
+                if (more < 1.f) S.den = -S.den;
+#pragma unroll
+                for (int d = 0; d < HD / 16; ++d) S.acc[d] *= rest;
+            }
             done(c0, S);
         }
     }
@@ -378,7 +414,7 @@ __device__ __forceinline__ Work find_work(const amusd_q8_cache& C, const Q8Segs&
 // A wave: a tile, one chunk.  Its sums go to memory.
 template <int HD, bool PER_TOKEN>
 __global__ void __launch_bounds__(64, HD == 64 ? 3 : 1) k_q8_att_part(amusd_q8_cache C, int layer, Q8Segs S, Q8Query Q) {
-    __shared__ float lds[2 * kMaxChunk];
+    __shared__ float lds[kWalkLds];
     const int kvh = blockIdx.x, tile = blockIdx.y, chunk = blockIdx.z, c0 = chunk * C.chunk;       // a kv head's waves on one XCD
     const Work W = find_work(C, S, layer, tile, kvh);
     if (c0 > W.last) return;
@@ -386,8 +422,8 @@ __global__ void __launch_bounds__(64, HD == 64 ? 3 : 1) k_q8_att_part(amusd_q8_c
     const Keys<HD> keys = load_keys<HD>(C, head, c0);
     const Scales sc = load_scales<PER_TOKEN>(C, head, c0);
     const Tile<HD> T = load_tile<HD>(C, Q, *W.seg, kvh, W.local);
-    const int lane = threadIdx.x, g = lane >> 4, pair = lane & 15;
     walk<HD, PER_TOKEN>(C, head, T, W.least, c0, min(c0 + C.chunk, (W.last + kStep) / kStep * kStep), keys, sc, lds, [&](int, const Sums<HD>& sums) {
+        const int lane = lane_anew(), g = lane >> 4, pair = lane & 15;
         float* out = C.part + (((size_t)tile * C.Hkv + kvh) * C.max_chunks + chunk) * ((HD + 2) * 16);
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d)
@@ -410,6 +446,7 @@ __global__ void __launch_bounds__(HD * 2) k_q8_att_merge(amusd_q8_cache C, Q8Seg
     constexpr int kAtOnce = 16, kRound = 64, kPart = (HD + 2) * 16, kThreadsOf = HD * 2;
     __shared__ float refs[kRound][16], dens[kRound][16], upto[kRound + 1][16];
     __shared__ v4f how[kRound][16];                          // what is done with a chunk: the sums before it times [0], its own times [1]; [2] its denominator
+    __shared__ int big[kThreadsOf / 64];                     // pairs (a bit each) with numerators that are kDown times what they are, of a wave's chunks
     const int kvh = blockIdx.x, tile = blockIdx.y, t = threadIdx.x;
     const Q8Seg& seg = S.s[find_seg(S, tile)];
     const int first = (tile - seg.unit0) * 16, pairs = min(16, seg.n * C.G - first);
@@ -418,6 +455,7 @@ __global__ void __launch_bounds__(HD * 2) k_q8_att_merge(amusd_q8_cache C, Q8Seg
     const int mine = chunks_of(min(pair, pairs - 1)), most = chunks_of(pairs - 1);
     const float* const part = C.part + ((size_t)tile * C.Hkv + kvh) * C.max_chunks * kPart;
     float ref = -INFINITY, den = 0.f, acc = 0.f;             // ref: the largest of the rounds before (threads 0 to 15)
+    bool down = false;
     for (int c0 = 0; c0 < most; c0 += kRound) {
         const int n = min(kRound, most - c0);
         float x[kAtOnce];
@@ -425,12 +463,22 @@ __global__ void __launch_bounds__(HD * 2) k_q8_att_merge(amusd_q8_cache C, Q8Seg
 #pragma unroll
             for (int i = 0; i < kAtOnce; ++i) x[i] = part[(size_t)min(from + i, most - 1) * kPart + col * 16 + pair];
         };
+        unsigned long long here = 0;
         for (int i = t; i < n * 32; i += kThreadsOf) {       // (references and denominators lie together)
             const float v = part[(size_t)(c0 + (i >> 5)) * kPart + HD * 16 + (i & 31)];
             (i & 16 ? dens : refs)[i >> 5][pair] = v;
+            here |= __ballot((i & 16) && v < 0.f && c0 + (i >> 5) < mine);
         }
+        if ((t & 63) == 0) big[t >> 6] = (int)((here >> 16 | here >> 48) & 0xFFFF);
         fetch(c0);
         __syncthreads();
+        int all_big = 0;
+#pragma unroll
+        for (int w = 0; w < kThreadsOf / 64; ++w) all_big |= big[w];
+        if (!down && (all_big >> pair & 1)) {
+            down = true;
+            acc *= kDown;
+        }
         if (t < 16) {
             upto[0][t] = ref;
             for (int c = 0; c < n; c += 16) {
@@ -449,7 +497,8 @@ __global__ void __launch_bounds__(HD * 2) k_q8_att_merge(amusd_q8_cache C, Q8Seg
             const int c = i >> 4;
             const float to = upto[c + 1][pair], at = to == -INFINITY ? 0.f : to;
             const float b = pow2(refs[c][pair] - at);
-            how[c][pair] = v4f{pow2(upto[c][pair] - at), b, dens[c][pair] * b, 0.f};
+            const float d = dens[c][pair];
+            how[c][pair] = v4f{pow2(upto[c][pair] - at), down && !(d < 0.f) ? b * kDown : b, fabsf(d) * b, 0.f};
         }
         __syncthreads();
         for (int c = 0; c < n; c += kAtOnce) {
@@ -468,13 +517,13 @@ __global__ void __launch_bounds__(HD * 2) k_q8_att_merge(amusd_q8_cache C, Q8Seg
     wait_vm<0>();
     if (pair >= pairs) return;
     const int row = (first + pair) / C.G, head = kvh * C.G + (first + pair) % C.G;
-    Q.out[(int64_t)(seg.row0 + row) * Q.ldo + (int64_t)head * HD + col] = q8_bf16(acc / den);
+    Q.out[(int64_t)(seg.row0 + row) * Q.ldo + (int64_t)head * HD + col] = q8_bf16(acc / den * (down ? 1.f / kDown : 1.f));
 }
 
 // A wave: a tile, all chunks.  The sums over the chunks so far wait in LDS, where they are touched once a chunk.
 template <int HD, bool PER_TOKEN>
 __global__ void __launch_bounds__(64, HD == 64 ? 3 : 2) k_q8_att_whole(amusd_q8_cache C, int layer, Q8Segs S, Q8Query Q) {
-    __shared__ float lds[2 * kMaxChunk];
+    __shared__ float lds[kWalkLds];
     __shared__ v4f all[HD / 16][64];
     const int kvh = blockIdx.x, lane = threadIdx.x;                             // a kv head's waves on one XCD, the longest first
     const Work W = find_work(C, S, layer, gridDim.y - 1 - blockIdx.y, kvh);
@@ -483,12 +532,14 @@ __global__ void __launch_bounds__(64, HD == 64 ? 3 : 2) k_q8_att_whole(amusd_q8_
     const Keys<HD> keys = load_keys<HD>(C, W.head, 0);
     const Scales sc = load_scales<PER_TOKEN>(C, W.head, 0);
     float ref = -INFINITY, den = 0.f;
+    bool down = false;
 #pragma unroll
     for (int d = 0; d < HD / 16; ++d) all[d][lane] = v4f{0.f, 0.f, 0.f, 0.f};
     walk<HD, PER_TOKEN>(C, W.head, T, W.least, 0, (W.last + kStep) / kStep * kStep, keys, sc, lds, [&](int c0, const Sums<HD>& part) {
         if (c0 > T.pos) return;                             // a chunk that the pair sees nothing of is not merged
+        const int lane = lane_anew();
         float a, b;
-        merge_weights(ref, den, part.ref, part.den, a, b);
+        merge_weights(ref, den, down, part.ref, part.den, a, b);
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d) {
             v4f v = all[d][lane];
@@ -499,14 +550,14 @@ __global__ void __launch_bounds__(64, HD == 64 ? 3 : 2) k_q8_att_whole(amusd_q8_
     });
     wait_vm<0>();
     if (T.pos < 0) return;
-    const int pair = W.local * 16 + (lane & 15);
-    uint16_t* out = Q.out + (int64_t)(W.seg->row0 + pair / C.G) * Q.ldo + (int64_t)(kvh * C.G + pair % C.G) * HD + (lane >> 4) * 4;
+    const int own = lane_anew(), pair = W.local * 16 + (own & 15);
+    uint16_t* out = Q.out + (int64_t)(W.seg->row0 + pair / C.G) * Q.ldo + (int64_t)(kvh * C.G + pair % C.G) * HD + (own >> 4) * 4;
 #pragma unroll
     for (int d = 0; d < HD / 16; ++d) {
         uint16_t b[4];
-        const v4f v = all[d][lane];
+        const v4f v = all[d][own];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) b[e] = q8_bf16(v[e] / den);
+        for (int e = 0; e < 4; ++e) b[e] = q8_bf16(v[e] / den * (down ? 1.f / kDown : 1.f));
         __builtin_memcpy(out + d * 16, b, 8);
     }
 }

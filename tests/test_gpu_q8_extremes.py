@@ -112,3 +112,98 @@ def test_quotients_past_127_in_the_cache(gpu, block):
     ref.append(0, _np(k) * np.repeat(size, 1, 1)[:, :, None])
     kk, _ = _read(gpu, cache, 0, 0, n, 2, hd)
     assert np.array_equal(kk, ref.values(n).astype(np.float32))
+
+
+# ---------------------------------------------------------------- attention
+def _filled(gpu, heads, n, k_std, v_std, seed=0, block=1, cap=None, k_edit=None, v_edit=None):
+    torch, A = gpu
+    hq, hkv, hd = heads
+    rng = np.random.default_rng([seed, hd, n])
+    k, v = (np.clip(rng.standard_normal((n, hkv, hd)) * std, -3.3e38, 3.3e38).astype(np.float32) for std in (k_std, v_std))
+    for a, edit in ((k, k_edit), (v, v_edit)):
+        if edit:
+            edit(a)
+    cache = A.Q8Cache(n_layers=1, n_seqs=1, n_q_heads=hq, n_kv_heads=hkv, head_dim=hd, capacity=cap or n, block=block)
+    bf = lambda a: torch.from_numpy(a).to(torch.bfloat16).cuda()   # noqa: E731
+    _append(gpu, cache, [0], [0], [bf(k)], [bf(v)])
+    return cache, rng
+
+
+def _held(gpu, cache, heads, n):
+    return (a.astype(np.float64) for a in _read(gpu, cache, 0, 0, n, heads[1], heads[2]))
+
+
+def _check_seen(gpu, cache, heads, q, pos0, scale, parts=True):
+    """All rows against float64, and a few of them in calls of their own: the same bits, whichever form takes them."""
+    torch, A = gpu
+    n = q.shape[0]
+    out, = _attend(gpu, cache, [0], [pos0], [q], scale)
+    k, v = _held(gpu, cache, heads, pos0 + n)
+    for lo in range(0, n, 64):
+        hi = min(n, lo + 64)
+        qn = _np(q)[lo:hi].astype(np.float64)
+        want, weighted, s = O.attention(qn, k, v, pos0 + lo, scale)
+        # (without the absolute 1e-30 of ordinary sizes; half a step of the smallest bf16 instead, which is four of float32's)
+        tol = _tolerance(qn, k, v, pos0 + lo, scale, want, weighted, s, False) - 1e-30 + 1.01 * 2.0 ** -134
+        err = np.abs(_np(out)[lo:hi].astype(np.float64) - want)
+        assert (err <= tol).all(), (lo, float((err / tol).max()))
+    if parts:
+        for lo, m in ((0, 1), (n - 1, 1), (n // 3, min(5, n - n // 3))):
+            part, = _attend(gpu, cache, [0], [pos0 + lo], [q[lo:lo + m]], scale)
+            assert torch.equal(part, out[lo:lo + m]), (lo, m)
+
+
+SHAPES = [((4, 2, 64), 300, 10, 1), ((8, 2, 128), 300, 4, 1), ((8, 2, 64), 600, 600, 1), ((8, 2, 128), 500, 500, 1), ((8, 1, 64), 400, 9, 32), ((8, 8, 128), 330, 330, 64),
+          ((4, 1, 64), 4500, 3, 1)]
+
+
+@pytest.mark.parametrize("heads,n,rows,block", SHAPES)
+@pytest.mark.parametrize("size", [1e31, 1e34, 1e35, 1e37, 3e38])
+def test_attention_of_large_values(gpu, heads, n, rows, block, size):
+    """3e38: of one sign as well, where the weighted sum before the division is past float32."""
+    torch, A = gpu
+
+    def edit(v):
+        if size == 3e38:
+            v[:] = np.abs(v)
+            v[..., ::5] = size
+        v[n // 2:n // 2 + 3] = 0
+    cache, rng = _filled(gpu, heads, n, 1.0, size / (8 if size == 3e38 else 1), block=block, v_edit=edit)
+    _check_seen(gpu, cache, heads, _rand(torch, rng, rows, heads[0], heads[2]), n - rows, heads[2] ** -0.5)
+
+
+@pytest.mark.parametrize("heads,n,rows,block", SHAPES)
+@pytest.mark.parametrize("first", [True, False])
+def test_attention_of_large_values_in_some_chunks(gpu, heads, n, rows, block, first):
+    """A stretch of large values behind, or in front of, ordinary ones."""
+    torch, A = gpu
+
+    def edit(v):
+        v[:n // 2 if first else n] *= 1e30
+        if not first:
+            v[:n // 2] *= 1e-30
+        v *= 1e6
+    cache, rng = _filled(gpu, heads, n, 1.0, 1.0, seed=1, block=block, v_edit=edit)
+    _check_seen(gpu, cache, heads, _rand(torch, rng, rows, heads[0], heads[2]), n - rows, heads[2] ** -0.5)
+
+
+@pytest.mark.parametrize("heads,n,rows,block", SHAPES)
+@pytest.mark.parametrize("size", [1e-28, 1e-33, 1e-36, 2e-38])
+def test_attention_of_small_values(gpu, heads, n, rows, block, size):
+    torch, A = gpu
+    cache, rng = _filled(gpu, heads, n, 1.0, size, seed=2, block=block)
+    _check_seen(gpu, cache, heads, _rand(torch, rng, rows, heads[0], heads[2]), n - rows, heads[2] ** -0.5)
+
+
+def test_attention_large_values_behind_a_row_change_nothing(gpu):
+    """What a row does not see moves neither its power of two nor its sums' scale, however large."""
+    torch, A = gpu
+    heads = (8, 2, 64)
+    for n, rows in ((40, 3), (220, 200)):
+        cache, rng = _filled(gpu, heads, n, 1.0, 1.0, seed=3, cap=512)
+        q = _rand(torch, rng, rows, 8, 64)
+        clean, = _attend(gpu, cache, [0], [n - rows], [q], 0.125)
+        bad = torch.full((100, 2, 64), 3e38, dtype=torch.bfloat16, device="cuda")
+        _append(gpu, cache, [0], [n], [bad], [bad])
+        again, = _attend(gpu, cache, [0], [n - rows], [q], 0.125)
+        assert torch.equal(clean, again)

@@ -30,6 +30,11 @@ typedef float f2 __attribute__((ext_vector_type(2)));
 
 constexpr int kPlane = 32512;                    // 127 * 256: a query's largest component in its 16 bits
 
+// Products of integers are below 2^29, so with a key's scale from kHugeKey on they could be past float32, whatever the query's factor.  Scales of a
+// chunk that holds one (seen or not: powers of two change no bits) are then taken down by kLowKey and the factor up, or the sums up again
+// where the factor is so large that the score itself is past it.
+constexpr float kHugeKey = 0x1p98f, kLowKey = 0x1p-24f, kLargeQs = 0x1p60f;
+
 struct Q8Query {                                 // a launch's constants
     const uint16_t* q;
     int64_t ldq;
@@ -44,6 +49,7 @@ template <int HD>
 struct Tile {
     uint4 hi[HD / 64], lo[HD / 64];
     float qs;                                    // score (in units of log2) per unit of the integer product, without the key's scale; positive
+    float low_qs;                                // .. for keys' scales that were taken down by kLowKey, where that is smaller than kLargeQs
     int pos;                                     // the pair's row's position (the last key that it sees); -1: no pair
 };
 
@@ -96,6 +102,7 @@ __device__ __forceinline__ Tile<HD> load_tile(const amusd_q8_cache& C, const Q8Q
     const float m = bad ? 0.f : __uint_as_float(most);
     const float inv = m > 0.f ? (float)kPlane / m : 0.f;
     T.qs = bad ? __uint_as_float(0x7FC00000u) : fmaxf(m / (float)kPlane * Q.scale2, 1.17549435e-38f);     // (not 0: 0 times -infinity)
+    T.low_qs = bad ? T.qs : fmaxf(m / (float)kPlane * (Q.scale2 * (1.f / kLowKey)), 1.17549435e-38f);
 #pragma unroll
     for (int f = 0; f < HD / 64; ++f) {
         uint32_t hi[4] = {}, lo[4] = {};
@@ -132,7 +139,8 @@ struct Sums {
 
 // Scales of a chunk's keys and values, 8 keys a lane: two loads of the wave have those of a longest chunk.
 constexpr int kMaxChunk = 512;
-constexpr int kWalkLds = 2 * kMaxChunk + 64;     // floats: a chunk's scales, and one of each lane's that is rarely read
+enum { kPost, kBack, kQs, kLowQs, kRare };            // what each lane keeps apart, as it is rarely read
+constexpr int kWalkLds = 2 * kMaxChunk + kRare * 64;     // floats: a chunk's scales, and that
 struct Scales {
     v4f k[2], v[2];
 };
@@ -216,12 +224,52 @@ __device__ __forceinline__ void step_scores(const Keys<HD>& K, const Tile<HD>& T
     }
 }
 
-// .. and its weights, as the values' product takes them, 2^lift (FAR: and post) times what they are.  MASK: some pair does not see all of
+// The lane, such that addresses made of it are found where they are used, once a chunk, and not kept in registers through its steps.
+__device__ __forceinline__ int lane_anew() {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
+__device__ __forceinline__ float& rare_of(float* lds, int what) { return lds[2 * kMaxChunk + what * 64 + lane_anew()]; }
+
+// .. and its weights, as the values' product takes them, 2^lift (RARE: and post) times what they are.  MASK: some pair does not see all of
 // its keys.  left: keys from the step's first one up to the last that the lane's pair sees.
-template <int HD, bool MASK, bool FAR>
-__device__ __forceinline__ void step_weights(float (&sc)[4][4], float qs, const v4f* vs, float lift, float post, int left, Sums<HD>& S, uint4 (&out)[2]) {
+template <int HD, bool MASK, bool RARE>
+__device__ __forceinline__ void step_exps(const float (&sc)[4][4], float qs, const v4f* vs, float lift, float post, int left, Sums<HD>& S, uint4 (&out)[2]) {
+    const int g4 = (threadIdx.x & 48) >> 2;
+    const float at = S.ref == -INFINITY ? 0.f : S.ref - lift;
+    float sum[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        v4f scale = vs[t * 4];
+        if (RARE) scale *= post;
+        float p[4], w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            p[e] = pow2(fmaf(sc[t][e], qs, -at));
+            w[e] = p[e] * scale[e];
+            if (MASK && t * 16 + g4 + e > left) w[e] = 0.f;          // (whatever its value's scale is)
+        }
+        sum[t] = (p[0] + p[1]) + (p[2] + p[3]);
+        auto two = [](float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, h2)); };
+        (t & 1 ? out[t >> 1].z : out[t >> 1].x) = two(w[0], w[1]);
+        (t & 1 ? out[t >> 1].w : out[t >> 1].y) = two(w[2], w[3]);
+    }
+    S.den += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+template <int HD, bool MASK>
+__device__ __forceinline__ void step_weights(float (&sc)[4][4], float qs, const v4f* vs, float lift, bool rare, float* lds, int left, Sums<HD>& S,
+                                             uint4 (&out)[2]) {
     const int g4 = (threadIdx.x & 48) >> 2;
     float top[4];
+    if (MASK && __builtin_expect(rare, 0)) {
+        const float back = rare_of(lds, kBack);
+        qs = rare_of(lds, kQs);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[t][e] *= back;
+    }
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
 #pragma unroll
@@ -241,25 +289,8 @@ __device__ __forceinline__ void step_weights(float (&sc)[4][4], float qs, const 
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d) S.acc[d] *= shrink;
     }
-    const float at = S.ref == -INFINITY ? 0.f : S.ref - lift;
-    float sum[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        v4f scale = vs[t * 4];
-        if (FAR) scale *= post;
-        float p[4], w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            p[e] = pow2(fmaf(sc[t][e], qs, -at));
-            w[e] = p[e] * scale[e];
-            if (MASK && t * 16 + g4 + e > left) w[e] = 0.f;          // (whatever its value's scale is)
-        }
-        sum[t] = (p[0] + p[1]) + (p[2] + p[3]);
-        auto two = [](float a, float b) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, h2)); };
-        (t & 1 ? out[t >> 1].z : out[t >> 1].x) = two(w[0], w[1]);
-        (t & 1 ? out[t >> 1].w : out[t >> 1].y) = two(w[2], w[3]);
-    }
-    S.den += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    if (!MASK || __builtin_expect(!rare, 1)) step_exps<HD, MASK, false>(sc, qs, vs, lift, 1.f, left, S, out);
+    else step_exps<HD, MASK, true>(sc, qs, vs, lift, rare_of(lds, kPost), left, S, out);
 }
 
 // sums so far and a chunk's: how both are weighed.  down: whether the numerators so far are kDown times what they are.
@@ -277,13 +308,6 @@ __device__ __forceinline__ void merge_weights(float& ref, float& den, bool& down
     }
 }
 
-// The lane, such that addresses made of it are found where they are used, once a chunk, and not kept in registers through its steps.
-__device__ __forceinline__ int lane_anew() {
-    int lane = threadIdx.x & 63;
-    asm volatile("" : "+v"(lane));
-    return lane;
-}
-
 // Walks the keys [begin, end) (multiples of a step; begin a chunk's) and calls done(chunk's first key, its sums) at the end of each chunk.
 // The next step's keys are fetched as soon as a step's scores are found, its values behind the values' product: into the registers that
 // those leave free.  least: the last key that all pairs see.
@@ -293,19 +317,19 @@ __device__ __forceinline__ void walk(const amusd_q8_cache& C, size_t kvh, const 
     const int g = (threadIdx.x & 63) >> 4;
     v4f* const kl = reinterpret_cast<v4f*>(lds);
     v4f* const vl = reinterpret_cast<v4f*>(lds + kMaxChunk);
-    auto post = [&]() -> float& { return lds[2 * kMaxChunk + lane_anew()]; };
+    rare_of(lds, kLowQs) = T.low_qs;
     Sums<HD> S;
     float lift = 0.f;
-    bool far = false;
-    int c0 = begin, plain = least;               // plain: the last key up to which steps are of the common kind
+    bool far = false;                            // the chunk's steps are of the rare kind
+    int c0 = begin, plain = least;               // plain: the last key up to which steps have nothing to mask, nor are of the rare kind
     auto chunk_begin = [&](int b) {
         c0 = b;
         const int lane = lane_anew(), g = lane >> 4;
         __builtin_amdgcn_wave_barrier();
-        float all = 0.f;
+        float all = 0.f, keys = 0.f;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            kl[i * 64 + lane] = sc.k[i];
+            keys = fmaxf(keys, fmaxf(fmaxf(sc.k[i][0], sc.k[i][1]), fmaxf(sc.k[i][2], sc.k[i][3])));
             vl[i * 64 + lane] = sc.v[i];
             all = fmaxf(all, fmaxf(fmaxf(sc.v[i][0], sc.v[i][1]), fmaxf(sc.v[i][2], sc.v[i][3])));
         }
@@ -328,9 +352,19 @@ __device__ __forceinline__ void walk(const amusd_q8_cache& C, size_t kvh, const 
         most = fmaxf(most, lane_xor<32>(most));
         const int all_of_it = most > 0.f ? 137 - (int)(__float_as_uint(most) >> 23) : 0, here = min(max(all_of_it, -kMaxLift), kMaxLift);
         lift = (float)here;
-        far = __any(all_of_it != here);
+        far = __any(keys >= kHugeKey || all_of_it != here);
         plain = far ? -1 : least;
-        if (far) post() = __uint_as_float((uint32_t)(127 + all_of_it - here) << 23);
+        if (__builtin_expect(far, 0)) {
+            const bool huge = __any(keys >= kHugeKey), low = T.qs < kLargeQs;
+            rare_of(lds, kPost) = __uint_as_float((uint32_t)(127 + all_of_it - here) << 23);
+            rare_of(lds, kBack) = huge && !low ? 1.f / kLowKey : 1.f;
+            rare_of(lds, kQs) = huge && low ? rare_of(lds, kLowQs) : T.qs;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) sc.k[i] *= huge ? kLowKey : 1.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) kl[i * 64 + lane] = sc.k[i];
+        __builtin_amdgcn_wave_barrier();
         S.ref = -INFINITY;
         S.den = 0.f;
         S.weights = v4f{0.f, 0.f, 0.f, 0.f};
@@ -348,9 +382,8 @@ __device__ __forceinline__ void walk(const amusd_q8_cache& C, size_t kvh, const 
         if (more) K = load_keys<HD>(C, kvh, b + kStep);
         if (ends && more) sc = load_scales<PER_TOKEN>(C, kvh, b + kStep);
         uint4 w[2];
-        if (b + kStep - 1 <= plain) step_weights<HD, false, false>(sc4, T.qs, vs, lift, 1.f, 0, S, w);
-        else if (__builtin_expect(!far, 1)) step_weights<HD, true, false>(sc4, T.qs, vs, lift, 1.f, T.pos - b, S, w);
-        else step_weights<HD, true, true>(sc4, T.qs, vs, lift, post(), T.pos - b, S, w);
+        if (b + kStep - 1 <= plain) step_weights<HD, false>(sc4, T.qs, vs, lift, false, lds, 0, S, w);
+        else step_weights<HD, true>(sc4, T.qs, vs, lift, far, lds, T.pos - b, S, w);
         const uint4 ones{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -378,7 +411,7 @@ __device__ __forceinline__ void walk(const amusd_q8_cache& C, size_t kvh, const 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) S.acc[d][e] = fmaf(-1152.f, S.weights[e], S.acc[d][e]) * down;
             if (__builtin_expect(far, 0)) {
-                const float more = post();
+                const float more = rare_of(lds, kPost);
                 const float rest = more < 1.f ? kDown / more : 1.f / more;          // (powers of two)
                 if (more < 1.f) S.den = -S.den;
 #pragma unroll

@@ -207,3 +207,12 @@ def test_attention_large_values_behind_a_row_change_nothing(gpu):
         _append(gpu, cache, [0], [n], [bad], [bad])
         again, = _attend(gpu, cache, [0], [n - rows], [q], 0.125)
         assert torch.equal(clean, again)
+
+
+@pytest.mark.parametrize("heads,n,rows,block", SHAPES)
+@pytest.mark.parametrize("qs,ks", [(1e-30, 1e30), (1e-32, 1e32), (1e-33, 1e34), (1e33, 1e-33), (1e36, 1e-37)])
+def test_attention_of_large_keys(gpu, heads, n, rows, block, qs, ks):
+    """Scores of ordinary size whose factors are not."""
+    torch, A = gpu
+    cache, rng = _filled(gpu, heads, n, ks, 1.0, seed=4, block=block)
+    _check_seen(gpu, cache, heads, _rand(torch, rng, rows, heads[0], heads[2], std=qs), n - rows, heads[2] ** -0.5)

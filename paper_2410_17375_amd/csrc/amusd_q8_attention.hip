@@ -30,10 +30,11 @@ typedef float f2 __attribute__((ext_vector_type(2)));
 
 constexpr int kPlane = 32512;                    // 127 * 256: a query's largest component in its 16 bits
 
-// Products of integers are below 2^29, so with a key's scale from kHugeKey on they could be past float32, whatever the query's factor.  Scales of a
-// chunk that holds one (seen or not: powers of two change no bits) are then taken down by kLowKey and the factor up, or the sums up again
-// where the factor is so large that the score itself is past it.
-constexpr float kHugeKey = 0x1p98f, kLowKey = 0x1p-24f, kLargeQs = 0x1p60f;
+// Products of integers are below 2^29, so with a key's scale of 2^99 they are past float32, whatever the query's factor; and a factor below
+// float32's normal numbers, which is held at the smallest of them, matters from a scale of 2^90 on.  Scales of a chunk that holds one from kHugeKey on
+// (seen or not: powers of two change no bits, but for keys 2^150 times smaller) are then taken down by kLowKey and the factor up, or the
+// sums up again where the factor is so large that the score itself is past float32.
+constexpr float kHugeKey = 0x1p64f, kLowKey = 0x1p-32f, kLargeQs = 0x1p60f;
 
 struct Q8Query {                                 // a launch's constants
     const uint16_t* q;
@@ -100,15 +101,18 @@ __device__ __forceinline__ Tile<HD> load_tile(const amusd_q8_cache& C, const Q8Q
     most = max(most, lane_xor_u<32>(most));
     const bool bad = most >= 0x7F800000u;
     const float m = bad ? 0.f : __uint_as_float(most);
-    const float inv = m > 0.f ? (float)kPlane / m : 0.f;
-    T.qs = bad ? __uint_as_float(0x7FC00000u) : fmaxf(m / (float)kPlane * Q.scale2, 1.17549435e-38f);     // (not 0: 0 times -infinity)
-    T.low_qs = bad ? T.qs : fmaxf(m / (float)kPlane * (Q.scale2 * (1.f / kLowKey)), 1.17549435e-38f);
+    // A largest component below 1e-34 has no finite reciprocal (kPlane times it): such queries are taken up first, by a power of two.
+    const float up = m < 0x1p-64f ? 0x1p64f : 1.f, step = m * up / (float)kPlane;
+    const float inv = m > 0.f ? (float)kPlane / (m * up) : 0.f;
+    // (the factors are not 0: 0 times -infinity)
+    T.qs = bad ? __uint_as_float(0x7FC00000u) : fmaxf(step * Q.scale2 / up, 1.17549435e-38f);
+    T.low_qs = bad ? T.qs : fmaxf(step * (Q.scale2 * (1.f / kLowKey / up)), 1.17549435e-38f);
 #pragma unroll
     for (int f = 0; f < HD / 64; ++f) {
         uint32_t hi[4] = {}, lo[4] = {};
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int v = bad ? 0 : min(max((int)rintf(x[f][i] * inv), -kPlane), kPlane);
+            const int v = bad ? 0 : min(max((int)rintf(x[f][i] * up * inv), -kPlane), kPlane);
             const int h = (v + 128) >> 8;
             hi[i / 4] |= (uint32_t)(h & 255) << (i % 4 * 8);
             lo[i / 4] |= (uint32_t)((v - h * 256) & 255) << (i % 4 * 8);

@@ -216,3 +216,13 @@ def test_attention_of_large_keys(gpu, heads, n, rows, block, qs, ks):
     torch, A = gpu
     cache, rng = _filled(gpu, heads, n, ks, 1.0, seed=4, block=block)
     _check_seen(gpu, cache, heads, _rand(torch, rng, rows, heads[0], heads[2], std=qs), n - rows, heads[2] ** -0.5)
+
+
+# ---------------------------------------------------------------- small queries
+@pytest.mark.parametrize("heads,n,rows,block", SHAPES)
+@pytest.mark.parametrize("qs,ks", [(1e-34, 1e34), (1e-36, 1e37), (1e-37, 1e36), (1e-38, 1e38)])
+def test_attention_of_small_queries(gpu, heads, n, rows, block, qs, ks):
+    """Queries whose 16 bits have no finite reciprocal in float32, against keys that give scores of ordinary size."""
+    torch, A = gpu
+    cache, rng = _filled(gpu, heads, n, ks, 1.0, seed=4, block=block)
+    _check_seen(gpu, cache, heads, _rand(torch, rng, rows, heads[0], heads[2], std=qs), n - rows, heads[2] ** -0.5)

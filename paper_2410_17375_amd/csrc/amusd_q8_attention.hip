@@ -234,6 +234,10 @@ __device__ __forceinline__ int lane_anew() {
     asm volatile("" : "+v"(lane));
     return lane;
 }
+// The reference is the largest product of a score and the factor, rounded; what the exponents are taken from is the product as it is (one
+// instruction).  From 2^24 on the two differ by 1 and more, from 2^30 by what a half cannot hold: such pairs' products are rounded too.
+__device__ __forceinline__ bool large_score(float ref) { return fabsf(ref) >= 0x1p23f && ref != -INFINITY; }
+
 __device__ __forceinline__ float& rare_of(float* lds, int what) { return lds[2 * kMaxChunk + what * 64 + lane_anew()]; }
 
 // .. and its weights, as the values' product takes them, 2^lift (RARE: and post) times what they are.  MASK: some pair does not see all of
@@ -242,6 +246,7 @@ template <int HD, bool MASK, bool RARE>
 __device__ __forceinline__ void step_exps(const float (&sc)[4][4], float qs, const v4f* vs, float lift, float post, int left, Sums<HD>& S, uint4 (&out)[2]) {
     const int g4 = (threadIdx.x & 48) >> 2;
     const float at = S.ref == -INFINITY ? 0.f : S.ref - lift;
+    const bool far = RARE && large_score(S.ref);
     float sum[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -250,7 +255,8 @@ __device__ __forceinline__ void step_exps(const float (&sc)[4][4], float qs, con
         float p[4], w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            p[e] = pow2(fmaf(sc[t][e], qs, -at));
+            const float x = fmaf(sc[t][e], qs, -at);
+            p[e] = pow2(far ? (sc[t][e] * qs - S.ref) + lift : x);
             w[e] = p[e] * scale[e];
             if (MASK && t * 16 + g4 + e > left) w[e] = 0.f;          // (whatever its value's scale is)
         }
@@ -262,7 +268,7 @@ __device__ __forceinline__ void step_exps(const float (&sc)[4][4], float qs, con
     S.den += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 template <int HD, bool MASK>
-__device__ __forceinline__ void step_weights(float (&sc)[4][4], float qs, const v4f* vs, float lift, bool rare, float* lds, int left, Sums<HD>& S,
+__device__ __forceinline__ void step_weights(float (&sc)[4][4], float qs, const v4f* vs, float lift, bool& rare, float* lds, int left, Sums<HD>& S,
                                              uint4 (&out)[2]) {
     const int g4 = (threadIdx.x & 48) >> 2;
     float top[4];
@@ -292,6 +298,12 @@ __device__ __forceinline__ void step_weights(float (&sc)[4][4], float qs, const 
         S.weights *= shrink;
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d) S.acc[d] *= shrink;
+        if (__builtin_expect(!rare && __any(large_score(ref)), 0)) {         // from here on the chunk's steps are of the rare kind
+            rare = true;
+            rare_of(lds, kPost) = rare_of(lds, kBack) = 1.f;
+            rare_of(lds, kQs) = qs;
+            return step_exps<HD, true, true>(sc, qs, vs, lift, 1.f, left, S, out);
+        }
     }
     if (!MASK || __builtin_expect(!rare, 1)) step_exps<HD, MASK, false>(sc, qs, vs, lift, 1.f, left, S, out);
     else step_exps<HD, MASK, true>(sc, qs, vs, lift, rare_of(lds, kPost), left, S, out);
@@ -325,7 +337,7 @@ __device__ __forceinline__ void walk(const amusd_q8_cache& C, size_t kvh, const 
     Sums<HD> S;
     float lift = 0.f;
     bool far = false;                            // the chunk's steps are of the rare kind
-    int c0 = begin, plain = least;               // plain: the last key up to which steps have nothing to mask, nor are of the rare kind
+    int c0 = begin;
     auto chunk_begin = [&](int b) {
         c0 = b;
         const int lane = lane_anew(), g = lane >> 4;
@@ -357,7 +369,6 @@ __device__ __forceinline__ void walk(const amusd_q8_cache& C, size_t kvh, const 
         const int all_of_it = most > 0.f ? 137 - (int)(__float_as_uint(most) >> 23) : 0, here = min(max(all_of_it, -kMaxLift), kMaxLift);
         lift = (float)here;
         far = __any(keys >= kHugeKey || all_of_it != here);
-        plain = far ? -1 : least;
         if (__builtin_expect(far, 0)) {
             const bool huge = __any(keys >= kHugeKey), low = T.qs < kLargeQs;
             rare_of(lds, kPost) = __uint_as_float((uint32_t)(127 + all_of_it - here) << 23);
@@ -386,7 +397,7 @@ __device__ __forceinline__ void walk(const amusd_q8_cache& C, size_t kvh, const 
         if (more) K = load_keys<HD>(C, kvh, b + kStep);
         if (ends && more) sc = load_scales<PER_TOKEN>(C, kvh, b + kStep);
         uint4 w[2];
-        if (b + kStep - 1 <= plain) step_weights<HD, false>(sc4, T.qs, vs, lift, false, lds, 0, S, w);
+        if (!far && b + kStep - 1 <= least) step_weights<HD, false>(sc4, T.qs, vs, lift, far, lds, kStep, S, w);
         else step_weights<HD, true>(sc4, T.qs, vs, lift, far, lds, T.pos - b, S, w);
         const uint4 ones{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
 #pragma unroll
@@ -509,13 +520,6 @@ __global__ void __launch_bounds__(HD * 2) k_q8_att_merge(amusd_q8_cache C, Q8Seg
         if ((t & 63) == 0) big[t >> 6] = (int)((here >> 16 | here >> 48) & 0xFFFF);
         fetch(c0);
         __syncthreads();
-        int all_big = 0;
-#pragma unroll
-        for (int w = 0; w < kThreadsOf / 64; ++w) all_big |= big[w];
-        if (!down && (all_big >> pair & 1)) {
-            down = true;
-            acc *= kDown;
-        }
         if (t < 16) {
             upto[0][t] = ref;
             for (int c = 0; c < n; c += 16) {
@@ -530,6 +534,13 @@ __global__ void __launch_bounds__(HD * 2) k_q8_att_merge(amusd_q8_cache C, Q8Seg
             }
         }
         __syncthreads();
+        int all_big = 0;
+#pragma unroll
+        for (int w = 0; w < kThreadsOf / 64; ++w) all_big |= big[w];
+        if (!down && (all_big >> pair & 1)) {
+            down = true;
+            acc *= kDown;
+        }
         for (int i = t; i < n * 16; i += kThreadsOf) {
             const int c = i >> 4;
             const float to = upto[c + 1][pair], at = to == -INFINITY ? 0.f : to;

@@ -226,3 +226,58 @@ def test_attention_of_small_queries(gpu, heads, n, rows, block, qs, ks):
     torch, A = gpu
     cache, rng = _filled(gpu, heads, n, ks, 1.0, seed=4, block=block)
     _check_seen(gpu, cache, heads, _rand(torch, rng, rows, heads[0], heads[2], std=qs), n - rows, heads[2] ** -0.5)
+
+
+# ---------------------------------------------------------------- large scores
+@pytest.mark.parametrize("heads,n,rows,block", SHAPES)
+@pytest.mark.parametrize("size", [300.0, 3e3, 1e4, 1e5, 1e8, 1e13, 1e17])
+def test_attention_of_large_scores(gpu, heads, n, rows, block, size):
+    """Scores up to float32's range, of either sign: a row whose largest is far above the others has its value."""
+    torch, A = gpu
+    hq, hkv, hd = heads
+    for sign in (0, -1):
+        def edit(k):
+            if sign:
+                k[:] = -np.abs(k) - size
+
+        cache, rng = _filled(gpu, heads, n, size, 1.0, seed=6, block=block, k_edit=edit)
+        q = _rand(torch, rng, rows, hq, hd, std=size)
+        q = torch.abs(q) if sign else q
+        out, = _attend(gpu, cache, [0], [n - rows], [q], hd ** -0.5)
+        k, v = _held(gpu, cache, heads, n)
+        qn = _np(q).astype(np.float64)
+        want, _, s = O.attention(qn, k, v, n - rows, hd ** -0.5)
+        # a score is off by the query's 16 bits and five roundings of float32 at most, of the sum of its terms' magnitudes
+        off = hd ** -0.5 * np.repeat(np.abs(k).sum(-1), hq // hkv, 1).T[None] * np.abs(qn).max(-1)[:, :, None] * (0.5 / 32512 + 7 * U32)
+        off = np.where(np.isfinite(s), off, 0).max(-1)
+        two = np.sort(s, -1)[..., -2:]                                       # (one row may see a single key: -inf below it)
+        clear = two[..., 1] - two[..., 0] > 2 * off + 30
+        assert clear.mean() > 0.5
+        err = np.abs(_np(out).astype(np.float64) - want)[clear]
+        # one weight; the others' are below e^-30.  Its value's half step in bf16; the weight times its value's scale to half (2^-11), where the
+        # denominator has the weight as it is; and the sums' with 1152 + v
+        assert (err <= ((U16 + 1.01 * 2.0 ** -11) * np.abs(want) + (8 * U32 * 1280 / 127 + n * np.exp(-30.0)) * np.abs(v).max())[clear]).all()
+        for lo, m in ((0, 1), (rows - 1, 1), (rows // 3, min(5, rows - rows // 3))):
+            part, = _attend(gpu, cache, [0], [n - rows + lo], [q[lo:lo + m]], hd ** -0.5)
+            assert torch.equal(part, out[lo:lo + m]), (lo, m)
+
+
+@pytest.mark.parametrize("heads,n,rows", [((4, 2, 64), 300, 10), ((8, 2, 128), 500, 500)])
+def test_attention_of_a_far_largest_score(gpu, heads, n, rows):
+    """Scores near 1e36: finite, and so far apart that the largest has all the weight."""
+    torch, A = gpu
+    hq, hkv, hd = heads
+
+    def edit(k):
+        k[3] = 1e36                                   # every row sees it
+    cache, rng = _filled(gpu, heads, n, 1.0, 1.0, seed=5, k_edit=edit)
+    q = torch.abs(_rand(torch, rng, rows, hq, hd)) + 0.5
+    if rows == n:
+        q[:3] = 0
+    out, = _attend(gpu, cache, [0], [n - rows], [q], hd ** -0.5)
+    _, v = _held(gpu, cache, heads, n)
+    want = np.repeat(v[3], hq // hkv, 0)
+    got = _np(out)[3 if rows == n else 0:].astype(np.float64)
+    # one weight: its value's half step in bf16; the weight times its value's scale to half (2^-11), where the denominator has the weight as
+    # it is; and the step that the chain of fp32 sums with 1152 + v leaves
+    assert (np.abs(got - want) <= (U16 + 1.01 * 2.0 ** -11) * np.abs(want) + 4 * U32 * 1280 / 127 * np.abs(v).max()).all()

@@ -300,7 +300,7 @@ int amusd_q8_quantize(const void *x, int32_t dtype, int64_t ldx, int32_t rows, i
                       float *scale, void *hip_stream);
 
 /* The RMS norm in front of a projection: s = x + add (add may be NULL; fp32 or bf16, add_dtype), sum = s in x's type (sum may
- * be NULL, or x itself), y = s / sqrt(mean(s^2) + eps) * gain, taken in 64 bits from s before that is rounded to
+ * be NULL, or x itself with its distance of rows; not add, and nothing that overlaps either otherwise), y = s / sqrt(mean(s^2) + eps) * gain, taken in 64 bits from s before that is rounded to
  * sum and rounded to float32, and y in 8 bits as amusd_q8_quantize has it.  gain: fp32 [n].  sum = x in bf16: n at most 16384. */
 int amusd_q8_rmsnorm(const void *x, int32_t dtype, int64_t ldx, const void *add, int32_t add_dtype, int64_t ldadd,
                      const float *gain, float eps, int32_t rows, int32_t n, void *sum, int64_t ldsum, int8_t *q,

@@ -642,6 +642,8 @@ int amusd_q8_rmsnorm(const void* x, int32_t dtype, int64_t ldx, const void* add,
     if (add && (!float_dtype(add_dtype) || ldadd < n || !aligned(add, add_dtype == AMUSD_DTYPE_BF16 ? 2 : 4)))
         return report(AMUSD_E_ARG, "q8_rmsnorm: bad rows to add");
     if (sum && (ldsum < n || !aligned(sum, dtype == AMUSD_DTYPE_BF16 ? 2 : 4))) return report(AMUSD_E_ARG, "q8_rmsnorm: bad rows for the sum");
+    // (rows longer than the registers read add a second time, after their sum was stored)
+    if (sum && sum == add) return report(AMUSD_E_ARG, "q8_rmsnorm: the sum takes the place of x or of neither");
     if (sum == x && sum && ldsum != ldx) return report(AMUSD_E_ARG, "q8_rmsnorm: the sum takes the place of x at another distance of rows");
     if (n > kQ8MaxRow && sum == x && dtype == AMUSD_DTYPE_BF16 && sum)
         return report(AMUSD_E_ARG, "q8_rmsnorm: a bf16 row of more than 16384 columns cannot be written over itself");

@@ -39,6 +39,16 @@ def test_rmsnorm(L):
         assert L.amusd_q8_rmsnorm(*{**good, **change}.values(), None) == 0
 
 
+def test_rmsnorm_sum_over_the_addend(L):
+    """add is read a second time where rows are longer than the registers: its place cannot take the sum, whatever its type."""
+    good = dict(x=P, dtype=0, ldx=32, add=P + 8192, add_dtype=0, ldadd=32, gain=P, eps=1e-5, rows=0, n=30, sum=NULL, ldsum=32, q=P, ldq=32, scale=P)
+    assert L.amusd_q8_rmsnorm(*good.values(), None) == 0
+    for change in (dict(), dict(add_dtype=1), dict(dtype=1, add_dtype=1), dict(n=20000, ldx=20000, ldadd=20000, ldsum=20000, ldq=20000)):
+        a = {**good, **change}
+        _refused(L.amusd_q8_rmsnorm(*{**a, "sum": a["add"]}.values(), None), L)
+        assert L.amusd_q8_rmsnorm(*{**a, "sum": P if a["dtype"] == 0 else P + 4}.values(), None) == 0
+
+
 def test_matrix_and_product(L):
     w = np.zeros((4, 64), np.float32).ctypes.data
     good = dict(w=w, dtype=0, scale=NULL, n=4, k=64, ld=64, gated=0, on_device=0, stream=NULL)

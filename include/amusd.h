@@ -329,7 +329,8 @@ int amusd_q8_gemm(const amusd_q8_matrix *w, const int8_t *x, int64_t ldx, const 
 
 /* The key-value caches of n_layers layers and n_seqs sequences in 8 bits, capacity positions each, with a scale for every `block`
  * positions (1, 16, 32 or 64) of a kv head's keys, and one of its values.  Also holds the memory that attention of few rows
- * needs.  Head counts and head_dim as in amusd_config; capacity at most 2^24, rounded up to a multiple of 64.  Zeroed. */
+ * needs: at most 128 MB or a 32nd of the cache, or what 16 rows need where that is more (131072 positions, 8 kv heads of
+ * 128, groups of 4: 324 MB with 16 sequences and more, 68 MB with one).  Head counts and head_dim as in amusd_config; capacity at most 2^24, rounded up to a multiple of 64.  Zeroed. */
 typedef struct amusd_q8_cache amusd_q8_cache;
 int amusd_q8_cache_create(int32_t n_layers, int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                           int32_t capacity, int32_t block, void *hip_stream, amusd_q8_cache **out);

@@ -59,6 +59,19 @@ inline bool attention_packs_rows(bool bf16, int head_dim, int group, int units, 
     return bf16 && head_dim == 64 && run_blocks < 8;
 }
 
+// Attention over an 8-bit cache: (tile of 16 pairs, kv head)s while which a tile's chunks are split over waves, and those whose sums there
+// is room for at a time: in 128 MB or a 32nd of the cache, but those of 16 rows always (of up to n_seqs sequences, whose last tiles
+// need not be full).  us, 64 rows of the 8B heads behind 131072 keys, 128 tiles together 462, 43 at a time 534, 32 at a time 586;
+// 100 rows a wave a tile 2159, 50 tiles at a time 807.
+inline int q8_split_tiles(int cus) { return cus * 5 / 4; }
+inline int q8_part_tiles(int n_seqs, int group, int kv_heads, int cus, int64_t tile_bytes, int64_t cache_bytes) {
+    const int segs = n_seqs < 16 ? n_seqs : 16;
+    const int64_t least = (int64_t)(16 * group + 15 * segs) / 16 * kv_heads, split = q8_split_tiles(cus);
+    const int64_t bytes = cache_bytes / 32 < 128 << 20 ? 128 << 20 : cache_bytes / 32, room = bytes / tile_bytes;
+    const int64_t most = split < room ? split : room;
+    return (int)(least > most ? least : most);
+}
+
 // Products of 8-bit integers: forms for few rows, whose workgroups' eight waves split the contraction of MT x 16 rows and NT x 16 features
 // (kQ8FewMTxNT), and for many, whose workgroups hold a tile of the result (kQ8Tile<features>x<rows>).
 enum Q8Form { kQ8Few1x1, kQ8Few1x2, kQ8Few2x2, kQ8Few2x4, kQ8Few4x4, kQ8Tile64, kQ8Tile128x64, kQ8Tile128, kQ8Tile256 };

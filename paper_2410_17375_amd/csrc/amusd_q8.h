@@ -29,7 +29,7 @@ struct amusd_q8_cache {
     int8_t* v = nullptr;           // [layer][seq][kv head][cap/32][hd/32][64 lanes][16]: q + 128 in operand order (q8_v_index)
     float* ks = nullptr;           // [layer][seq][kv head][cap/block]
     float* vs = nullptr;
-    float* part = nullptr;         // [part_tiles][max_chunks][hd + 2][16]: numerators, reference, denominator of 16 pairs
+    float* part = nullptr;         // [part_tiles][max_chunks][hd + 2][16]: numerators, reference, denominator of 16 pairs (part_tiles: q8_part_tiles)
 };
 
 namespace amusd {

@@ -461,9 +461,9 @@ __device__ __forceinline__ Work find_work(const amusd_q8_cache& C, const Q8Segs&
 
 // A wave: a tile, one chunk.  Its sums go to memory.
 template <int HD, bool PER_TOKEN>
-__global__ void __launch_bounds__(64, HD == 64 ? 3 : 1) k_q8_att_part(amusd_q8_cache C, int layer, Q8Segs S, Q8Query Q) {
+__global__ void __launch_bounds__(64, HD == 64 ? 3 : 1) k_q8_att_part(amusd_q8_cache C, int layer, Q8Segs S, Q8Query Q, int tile0) {
     __shared__ float lds[kWalkLds];
-    const int kvh = blockIdx.x, tile = blockIdx.y, chunk = blockIdx.z, c0 = chunk * C.chunk;       // a kv head's waves on one XCD
+    const int kvh = blockIdx.x, tile = tile0 + blockIdx.y, chunk = blockIdx.z, c0 = chunk * C.chunk;       // a kv head's waves on one XCD
     const Work W = find_work(C, S, layer, tile, kvh);
     if (c0 > W.last) return;
     const size_t head = W.head;
@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(64, HD == 64 ? 3 : 1) k_q8_att_part(amusd_q8_c
     const Tile<HD> T = load_tile<HD>(C, Q, *W.seg, kvh, W.local);
     walk<HD, PER_TOKEN>(C, head, T, W.least, c0, min(c0 + C.chunk, (W.last + kStep) / kStep * kStep), keys, sc, lds, [&](int, const Sums<HD>& sums) {
         const int lane = lane_anew(), g = lane >> 4, pair = lane & 15;
-        float* out = C.part + (((size_t)tile * C.Hkv + kvh) * C.max_chunks + chunk) * ((HD + 2) * 16);
+        float* out = C.part + (((size_t)blockIdx.y * C.Hkv + kvh) * C.max_chunks + chunk) * ((HD + 2) * 16);
 #pragma unroll
         for (int d = 0; d < HD / 16; ++d)
 #pragma unroll
@@ -490,18 +490,18 @@ __device__ __forceinline__ uint16_t q8_bf16(float v) { return __builtin_bit_cast
 // A workgroup merges HD / 8 columns of a tile: thread (column, pair).  How each chunk is weighed follows from the references alone: found
 // for up to 64 chunks at a time by as many threads, while the sums are on their way; those are then added up in order.
 template <int HD>
-__global__ void __launch_bounds__(HD * 2) k_q8_att_merge(amusd_q8_cache C, Q8Segs S, Q8Query Q) {
+__global__ void __launch_bounds__(HD * 2) k_q8_att_merge(amusd_q8_cache C, Q8Segs S, Q8Query Q, int tile0) {
     constexpr int kAtOnce = 16, kRound = 64, kPart = (HD + 2) * 16, kThreadsOf = HD * 2;
     __shared__ float refs[kRound][16], dens[kRound][16], upto[kRound + 1][16];
     __shared__ v4f how[kRound][16];                          // what is done with a chunk: the sums before it times [0], its own times [1]; [2] its denominator
     __shared__ int big[kThreadsOf / 64];                     // pairs (a bit each) with numerators that are kDown times what they are, of a wave's chunks
-    const int kvh = blockIdx.x, tile = blockIdx.y, t = threadIdx.x;
+    const int kvh = blockIdx.x, tile = tile0 + blockIdx.y, t = threadIdx.x;
     const Q8Seg& seg = S.s[find_seg(S, tile)];
     const int first = (tile - seg.unit0) * 16, pairs = min(16, seg.n * C.G - first);
     const int pair = t & 15, col = blockIdx.z * (HD / 8) + (t >> 4);
     auto chunks_of = [&](int p) { return (seg.pos0 + (first + p) / C.G) / C.chunk + 1; };
     const int mine = chunks_of(min(pair, pairs - 1)), most = chunks_of(pairs - 1);
-    const float* const part = C.part + ((size_t)tile * C.Hkv + kvh) * C.max_chunks * kPart;
+    const float* const part = C.part + ((size_t)blockIdx.y * C.Hkv + kvh) * C.max_chunks * kPart;
     float ref = -INFINITY, den = 0.f, acc = 0.f;             // ref: the largest of the rounds before (threads 0 to 15)
     bool down = false;
     for (int c0 = 0; c0 < most; c0 += kRound) {
@@ -619,11 +619,8 @@ void q8_attention_plan(amusd_q8_cache& c) {
     while (chunk < kMaxChunk && (int64_t)c.cap / chunk * c.Hkv > c.cus / 2) chunk *= 2;
     c.chunk = chunk;
     c.max_chunks = (c.cap + chunk - 1) / chunk;
-    // Tiles whose chunks are split over waves: while there are fewer than five for four compute units (8B shape, 100 rows behind 1000 keys, 200
-    // tiles: 21 us against 29 for a wave a tile; 250 rows, 504 tiles: 43 against 34).  64 MB of sums at most, but those of 16 rows always.
-    const int64_t tile_bytes = (int64_t)c.max_chunks * (c.hd + 2) * 16 * 4;
-    const int64_t least = (kMaxSegs + (kMaxSegs * c.G + 15) / 16) * (int64_t)c.Hkv;
-    c.part_tiles = (int)std::max(least, std::min<int64_t>(c.cus * 5 / 4, (64 << 20) / tile_bytes));
+    c.part_tiles = q8_part_tiles(c.n_seqs, c.G, c.Hkv, c.cus, (int64_t)c.max_chunks * (c.hd + 2) * 16 * 4,
+                                 (int64_t)c.n_layers * c.n_seqs * c.Hkv * c.cap * 2 * c.hd);
 }
 
 hipError_t launch_q8_attention(const amusd_q8_cache& c, int layer, const Q8Segs& segs, const void* q, int64_t ldq, float scale, const float* cos,
@@ -638,10 +635,16 @@ hipError_t launch_q8_attention(const amusd_q8_cache& c, int layer, const Q8Segs&
     auto go = [&](auto hd, auto per_token) {
         constexpr int HD = decltype(hd)::value;
         constexpr bool PT = decltype(per_token)::value;
-        if (tiles * c.Hkv <= c.part_tiles) {
-            const int chunks = (S.max_len + c.chunk - 1) / c.chunk;
-            hipLaunchKernelGGL((k_q8_att_part<HD, PT>), dim3(c.Hkv, (unsigned)tiles, chunks), dim3(64), 0, stream, c, layer, S, Q);
-            hipLaunchKernelGGL((k_q8_att_merge<HD>), dim3(c.Hkv, (unsigned)tiles, 8), dim3(HD * 2), 0, stream, c, S, Q);
+        // Chunks are split over waves while there are fewer than five tiles for four compute units (8B shape, 100 rows behind 1000 keys, 200
+        // tiles: 21 us against 29 for a wave a tile; 250 rows, 504 tiles: 43 against 34), or what 16 rows have; as many at a time as there is room for.
+        if (tiles * c.Hkv <= std::max(c.part_tiles, q8_split_tiles(c.cus))) {
+            const int chunks = (S.max_len + c.chunk - 1) / c.chunk, most = c.part_tiles / c.Hkv, turns = ((int)tiles + most - 1) / most;
+            const int per = ((int)tiles + turns - 1) / turns;
+            for (int at = 0; at < tiles; at += per) {
+                const unsigned n = (unsigned)std::min(per, (int)tiles - at);
+                hipLaunchKernelGGL((k_q8_att_part<HD, PT>), dim3(c.Hkv, n, chunks), dim3(64), 0, stream, c, layer, S, Q, at);
+                hipLaunchKernelGGL((k_q8_att_merge<HD>), dim3(c.Hkv, n, 8), dim3(HD * 2), 0, stream, c, S, Q, at);
+            }
         } else {
             hipLaunchKernelGGL((k_q8_att_whole<HD, PT>), dim3(c.Hkv, (unsigned)tiles), dim3(64), 0, stream, c, layer, S, Q);
         }

@@ -1,0 +1,54 @@
+"""The 8-bit cache and its attention at long capacities: the memory that it takes beside keys and values, and calls whose chunk sums go through that
+memory a part at a time."""
+import numpy as np
+import pytest
+
+from test_gpu_q8 import _attend, gpu  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _long_cache(gpu, heads, capacity, n_seqs, base, rows, block=1, seed=0):
+    """Sequences with 300 early positions and `rows` behind `base`; what lies between are zeros."""
+    torch, A = gpu
+    hq, hkv, hd = heads
+    cache = A.Q8Cache(n_layers=1, n_seqs=n_seqs, n_q_heads=hq, n_kv_heads=hkv, head_dim=hd, capacity=capacity, block=block)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    normal = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(torch.bfloat16)   # noqa: E731
+    qs = []
+    for i in range(n_seqs):
+        for at, n in ((0, 300), (base - 50, 50 + rows)):
+            k, v = normal(n, hkv * hd), normal(n, hkv * hd)
+            cache.append(0, [i], [at], [n], k.data_ptr(), v.data_ptr(), hkv * hd)
+        qs.append(normal(rows, hq, hd))
+    torch.cuda.synchronize()
+    return cache, qs
+
+
+@pytest.mark.parametrize("n_seqs", [1, 3])
+def test_memory_beside_keys_and_values(gpu, n_seqs):
+    torch, A = gpu
+    capacity, heads, hd = 1 << 17, 8, 128
+    _long_cache(gpu, (4, 2, 64), 512, 1, 400, 3)[0].free()          # (the first calls of a process take memory for its programs)
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    cache = A.Q8Cache(n_layers=1, n_seqs=n_seqs, n_q_heads=4 * heads, n_kv_heads=heads, head_dim=hd, capacity=capacity)
+    taken = free - torch.cuda.mem_get_info()[0]
+    cache.free()
+    held = 2 * n_seqs * heads * capacity * (hd + 4)
+    # Room for sums: 128 MB or a 32nd, or what 16 rows have.  Chunks of 512 keys, a tile's sums (hd + 2) * 16 floats each: 16 rows of 4 heads are 4 tiles, and a part of one more for each sequence
+    sums = (64 + 15 * n_seqs) // 16 * heads * (capacity // 512) * (hd + 2) * 64
+    assert held <= taken <= held + max(sums, 128 << 20, held // 32) + (16 << 20)
+
+
+@pytest.mark.parametrize("heads,n_seqs,rows", [((32, 8, 128), 1, 80), ((8, 1, 64), 3, 90), ((16, 8, 64), 2, 65)])
+def test_sums_a_part_at_a_time(gpu, heads, n_seqs, rows):
+    """Rows whose sums do not fit the room together, against the same rows 7 at a time."""
+    torch, A = gpu
+    capacity, base = 1 << 17, (1 << 17) - 200
+    cache, qs = _long_cache(gpu, heads, capacity, n_seqs, base, rows)
+    whole = _attend(gpu, cache, list(range(n_seqs)), [base] * n_seqs, qs, heads[2] ** -0.5)
+    for i, q in enumerate(qs):
+        for lo in range(0, rows, 7):
+            part, = _attend(gpu, cache, [i], [base + lo], [q[lo:lo + 7]], heads[2] ** -0.5)
+            assert torch.equal(part, whole[i][lo:lo + 7]), (i, lo)

@@ -19,6 +19,15 @@ def test_choice_of_a_products_form(tmp_path):
     assert r.returncode == 0, r.stdout
 
 
+def test_room_for_attentions_sums(tmp_path):
+    exe = str(tmp_path / "q8_tiles_test")
+    src = os.path.join(ROOT, "tests", "cpu", "q8_tiles_test.cpp")
+    r = subprocess.run(["g++", "-std=c++17", "-O2", src, "-o", exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stdout
+
+
 @pytest.mark.parametrize("source", ["amusd_q8.hip", "amusd_q8_gemm.hip", "amusd_q8_attention.hip"])
 def test_kernels_keep_to(tmp_path, source):
     kernels = _compile(os.path.join(CSRC, source), tmp_path / "q8.s")

@@ -56,7 +56,8 @@ extern "C" {
 #define AMUSD_DTYPE_INT8    2   /* an 8-bit model: tensors come in bf16 as with AMUSD_DTYPE_BF16, matrices and cache are held as signed 8 bits with
                                   * fp32 scales (a feature, a position and kv head), embedding and gains as they are.  A pass is the 8-bit operators
                                   * below one after the other.  It is another model than the bf16 one of the same tensors, and keeps
-                                  * the same promises: exact loops, rows whose bits depend on their sequence alone.  Widths are at
+                                  * the same promises: exact loops, rows whose bits depend on their sequence alone (among models of
+                                  * one max_ctx: attention's chunks follow from it, amusd_q8_attention).  Widths are at
                                   * most 131072, max_ctx 2^24 (else ARG) */
 #define AMUSD_MAX_K        16   /* rows of one pass: the 16-row matrix-core tile */
 #define AMUSD_MAX_SEQS   4096   /* sequences (key-value caches) one model can hold */
@@ -354,8 +355,10 @@ int amusd_q8_cache_read(const amusd_q8_cache *c, int32_t layer, int32_t n_seq, c
 /* Causal attention: row j of sequence seq_ids[i] stands at position pos0[i] + j and sees that sequence's positions up to its own,
  * which have to be in the cache (its own too).  out = softmax(scale * q . k) v, q and out bf16 rows
  * [n_q_heads * head_dim], q turned by the tables as keys are.  A query is rounded to 16 bits of its largest
- * component, softmax weights to 11 bits; sums are fp32.  A row's bits depend on its query and on what it sees, not on the
- * call's other rows.  A call's rows times n_q_heads / n_kv_heads are at most 2^19. */
+ * component, a softmax weight times its value's scale to 11 bits or 2^-35 of the largest scale that the row sees among its
+ * chunk's; sums are fp32, and scores have to be inside of it.  A row's bits depend on its query and on what it sees, not on the
+ * call's other rows; and on the chunks of keys whose sums are merged, 64 to 512 by the cache's capacity times
+ * its kv heads and the device's compute units (256 of them: 64 up to 8192, 128 up to about 16384, 256 up to about 32768, else 512).  A call's rows times n_q_heads / n_kv_heads are at most 2^19. */
 int amusd_q8_attention(amusd_q8_cache *c, int32_t layer, int32_t n_seq, const int32_t *seq_ids, const int32_t *pos0,
                        const int32_t *n, const void *q, int64_t ldq, float scale, const float *rope_cos,
                        const float *rope_sin, void *out, int64_t ldo, void *hip_stream);

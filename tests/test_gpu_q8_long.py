@@ -41,6 +41,25 @@ def test_memory_beside_keys_and_values(gpu, n_seqs):
     assert held <= taken <= held + max(sums, 128 << 20, held // 32) + (16 << 20)
 
 
+@pytest.mark.parametrize("heads,capacities", [((8, 2, 64), (700, 2048, 4096)), ((8, 2, 128), (4160, 8192)), ((4, 4, 64), (4352, 8192)), ((16, 8, 128), (4608, 70000))])
+def test_capacities_with_one_chunk_give_one_result(gpu, heads, capacities):
+    """Bits follow from the chunks, and these from the capacity times the kv heads (on 256 compute units: up to 8192, 16384, 32768, more)."""
+    torch, A = gpu
+    if torch.cuda.get_device_properties(0).multi_processor_count != 256:
+        pytest.skip("the capacities are those of 256 compute units")
+    hq, hkv, hd = heads
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    k, v = (torch.randn(690, hkv * hd, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(300, hq, hd, generator=gen, device="cuda").to(torch.bfloat16)
+    got = []
+    for capacity in capacities:
+        cache = A.Q8Cache(n_layers=1, n_seqs=1, n_q_heads=hq, n_kv_heads=hkv, head_dim=hd, capacity=capacity)
+        cache.append(0, [0], [0], [690], k.data_ptr(), v.data_ptr(), hkv * hd)
+        got.append([_attend(gpu, cache, [0], [690 - n], [q[:n]], hd ** -0.5)[0] for n in (1, 9, 300)])
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
 @pytest.mark.parametrize("heads,n_seqs,rows", [((32, 8, 128), 1, 80), ((8, 1, 64), 3, 90), ((16, 8, 64), 2, 65)])
 def test_sums_a_part_at_a_time(gpu, heads, n_seqs, rows):
     """Rows whose sums do not fit the room together, against the same rows 7 at a time."""

@@ -313,12 +313,24 @@ def q8_rmsnorm(x, dtype, ldx, add, add_dtype, ldadd, gain, eps, rows, n, sum, ld
 
 
 class Q8Matrix:
-    """Handle of one amusd_q8_matrix.  w (and scale, with 8-bit weights): numpy arrays (host) or device addresses."""
+    """Handle of one amusd_q8_matrix.  w (and scale, with 8-bit weights): numpy arrays (host) or device addresses.  A host array holds what the
+    call reads: n rows of k elements of dtype's size at a distance of ld."""
 
     def __init__(self, w, dtype, n, k, scale=None, ld=None, gated=False, on_device=False, stream=0):
         if not on_device:
-            w = np.ascontiguousarray(w)
+            w, at = np.asarray(w), k if ld is None else ld
+            size = {DTYPE_FP32: 4, DTYPE_BF16: 2, DTYPE_INT8: 1}.get(dtype, w.itemsize)
+            if w.itemsize != size:
+                raise ValueError(f"w has elements of {w.itemsize} bytes, its dtype {size}")
+            if w.shape != (n, k) or w.strides != (at * size, size):        # (rows of a wider array are read where they are)
+                if ld is not None and not w.flags.c_contiguous:
+                    raise ValueError("w is not the rows that ld says")
+                w = np.ascontiguousarray(w)
+                if w.size < (n - 1) * at + k:
+                    raise ValueError(f"w has {w.size} elements: fewer than its rows")
             keep = None if scale is None else np.ascontiguousarray(scale, dtype=np.float32)
+            if keep is not None and keep.size < n:
+                raise ValueError(f"{keep.size} scales for {n} features")
             ptr, scale = w.ctypes.data, 0 if keep is None else keep.ctypes.data
         else:
             ptr = int(w)

@@ -62,6 +62,25 @@ def test_matrix_and_product(L):
     assert L.amusd_q8_gemm(None, P, 64, P, 1, P, 0, 4, None, 0, None) == -1
 
 
+def test_matrix_of_a_host_array(L):
+    """The binding hands over no array that is shorter than what the call reads, nor one whose rows lie otherwise."""
+    import paper_2410_17375_amd as A
+    w, s = np.zeros((4, 64), np.float32), np.ones(4, np.float32)
+    for bad in (dict(n=5), dict(k=65), dict(n=4, k=60, ld=66), dict(dtype=A.DTYPE_BF16), dict(w=w.astype(np.float64)), dict(w=w[:, :60], k=60, ld=60),
+                dict(w=w[:, ::2], k=32, ld=64), dict(w=w.T, n=64, k=4, ld=64), dict(w=w.astype(np.int8), dtype=A.DTYPE_INT8, scale=s[:3]), dict(w=w[:3]),
+                dict(w=w[0], n=2, k=33)):
+        with pytest.raises(ValueError):
+            A.Q8Matrix(**{**dict(w=w, dtype=A.DTYPE_FP32, n=4, k=64), **bad})
+    # these get past the binding: refused for want of a device (here), or for what the call itself refuses
+    torch = pytest.importorskip("torch")
+    if torch.cuda.is_available():
+        return
+    for good in (dict(), dict(n=3), dict(w=w[:, :60], k=60, ld=64), dict(w=w[:, :60], k=60), dict(w=w.T, n=64, k=4), dict(w=w.reshape(-1), ld=64), dict(n=0), dict(dtype=7),
+                 dict(w=w.astype(np.int8), dtype=A.DTYPE_INT8, scale=s)):
+        with pytest.raises(A.AmusdError):
+            A.Q8Matrix(**{**dict(w=w, dtype=A.DTYPE_FP32, n=4, k=64), **good})
+
+
 def test_cache(L):
     good = dict(n_layers=1, n_seqs=1, n_q_heads=8, n_kv_heads=2, head_dim=64, capacity=64, block=1, stream=NULL)
     h = C.c_void_p()

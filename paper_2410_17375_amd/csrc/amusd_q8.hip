@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(1024) k_q8_rows(const X* x, int64_t ldx, const
             for (int i = 0; i < kHeld; ++i)
                 if (first + i * stride < n) f(i, first + i * stride);
         } else {
-            for (int at = first; at < n; at += stride) f(0, at);
+            for (unsigned at = first; at < (unsigned)n; at += stride) f(0, (int)at);       // (past the end of a longest row: 2^31 and more)
         }
     };
     auto fetch = [&](int i, int at, bool summed) {                   // summed: what is in x's place is the sum already
@@ -209,7 +209,7 @@ static void q8_rows(const void* x, int64_t ldx, const void* add, int64_t ldadd, 
     // 6.2); four for many and long ones, for more workgroups a compute unit, in different phases (2048 x 14336 22.8 us for 25.4; 2048 x 4096 and
     // x 8192 10.4 for 9.4 and 15.9 for 15.3).  A norm has two whatever the number of rows: its sum of squares has its order from that.
     const int vectors = NORM ? 2 : rows <= 128 ? 1 : rows > 1024 && n > 8 * 1024 ? 4 : 2;
-    const int threads = std::min(1024, std::max(64, (n + vectors * 512 - 1) / (vectors * 512) * 64));
+    const int threads = (int)std::min<int64_t>(1024, ((int64_t)n + vectors * 512 - 1) / (vectors * 512) * 64);
     auto launch = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3(rows), dim3(threads), 0, stream, static_cast<const X*>(x), ldx, static_cast<const A*>(add), ldadd, gain, eps, n,
                            static_cast<X*>(sum), ldsum, q, ldq, scale);

@@ -71,3 +71,29 @@ def test_sums_a_part_at_a_time(gpu, heads, n_seqs, rows):
         for lo in range(0, rows, 7):
             part, = _attend(gpu, cache, [i], [base + lo], [q[lo:lo + 7]], heads[2] ** -0.5)
             assert torch.equal(part, whole[i][lo:lo + 7]), (i, lo)
+
+
+def test_rows_of_2_31_columns(gpu):
+    """The longest rows that a call takes: positions behind the last one are past 31 bits."""
+    torch, A = gpu
+    n, part = 2 ** 31 - 1, 1 << 27
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(n, dtype=torch.bfloat16, device="cuda")
+    for lo in range(0, n, part):
+        x[lo:lo + part] = torch.randn(min(part, n - lo), generator=gen, device="cuda")
+    q = torch.full((n + 17,), 99, dtype=torch.int8, device="cuda")
+    s = torch.empty(1, device="cuda")
+    A.q8_quantize(x.data_ptr(), A.DTYPE_BF16, n, 1, n, q.data_ptr(), n + 1, s.data_ptr())
+    torch.cuda.synchronize()
+    most = max(x[lo:lo + part].abs().max().item() for lo in range(0, n, part))
+    assert s.item() == np.float32(np.float64(most) / 127)
+    for lo in range(0, n, part):
+        assert torch.equal(q[lo:lo + part][:n - lo].float(), torch.round(x[lo:lo + part].float() / s)), lo
+    assert (q[n:] == 99).all().item()
+    gain = torch.ones(n, device="cuda")
+    A.q8_rmsnorm(x.data_ptr(), A.DTYPE_BF16, n, 0, 0, 0, gain.data_ptr(), 0.0, 1, n, 0, 0, q.data_ptr(), n + 1, s.data_ptr())
+    torch.cuda.synchronize()
+    mean = sum((x[lo:lo + part].double() ** 2).sum().item() for lo in range(0, n, part)) / n
+    # the element's rounding and the scale's, 2^-24 each, and 2^31 sums of 2^-53
+    assert abs(s.item() / (most / mean ** 0.5 / 127) - 1) <= 2 * 2.0 ** -24 + 2 * 2.0 ** -22
+    assert (q[n:] == 99).all().item()

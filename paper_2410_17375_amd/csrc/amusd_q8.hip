@@ -210,9 +210,13 @@ static void q8_rows(const void* x, int64_t ldx, const void* add, int64_t ldadd, 
     // x 8192 10.4 for 9.4 and 15.9 for 15.3).  A norm has two whatever the number of rows: its sum of squares has its order from that.
     const int vectors = NORM ? 2 : rows <= 128 ? 1 : rows > 1024 && n > 8 * 1024 ? 4 : 2;
     const int threads = (int)std::min<int64_t>(1024, ((int64_t)n + vectors * 512 - 1) / (vectors * 512) * 64);
+    // (a launch of 2^32 threads and more ends without an error and without its last workgroups)
+    const int most = (int)(0xFFFFFFFFu / threads);
     auto launch = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(rows), dim3(threads), 0, stream, static_cast<const X*>(x), ldx, static_cast<const A*>(add), ldadd, gain, eps, n,
-                           static_cast<X*>(sum), ldsum, q, ldq, scale);
+        for (int64_t r = 0; r < rows; r += most)
+            hipLaunchKernelGGL(kernel, dim3(std::min<int64_t>(most, rows - r)), dim3(threads), 0, stream, static_cast<const X*>(x) + r * ldx, ldx,
+                               add ? static_cast<const A*>(add) + r * ldadd : nullptr, ldadd, gain, eps, n, sum ? static_cast<X*>(sum) + r * ldsum : nullptr,
+                               ldsum, q + r * ldq, ldq, scale + r);
     };
     if (n <= 8 * threads) launch(k_q8_rows<X, A, NORM, 1>);
     else if (n <= 2 * 8 * threads) launch(k_q8_rows<X, A, NORM, 2>);

@@ -97,3 +97,20 @@ def test_rows_of_2_31_columns(gpu):
     # the element's rounding and the scale's, 2^-24 each, and 2^31 sums of 2^-53
     assert abs(s.item() / (most / mean ** 0.5 / 127) - 1) <= 2 * 2.0 ** -24 + 2 * 2.0 ** -22
     assert (q[n:] == 99).all().item()
+
+
+def test_more_rows_than_a_launch_takes(gpu):
+    """2^26 rows of a wave each are 2^32 threads."""
+    torch, A = gpu
+    rows = (1 << 26) + 37
+    x = torch.arange(rows, dtype=torch.int32, device="cuda").remainder_(1013).float() - 500
+    q, s = torch.full((rows, 16), 99, dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+    A.q8_quantize(x.data_ptr(), A.DTYPE_FP32, 1, rows, 1, q.data_ptr(), 16, s.data_ptr())
+    torch.cuda.synchronize()
+    assert torch.equal(q[:, 0].float(), 127 * torch.sign(x)) and (q[:, 1:] == 99).all().item()
+    assert torch.equal(s, torch.abs(x) / torch.full_like(x, 127))
+    gain = torch.ones(1, device="cuda")
+    y = torch.empty(rows, device="cuda")
+    A.q8_rmsnorm(x.data_ptr(), A.DTYPE_FP32, 1, x.data_ptr(), A.DTYPE_FP32, 1, gain.data_ptr(), 1e-5, rows, 1, y.data_ptr(), 1, q.data_ptr(), 16, s.data_ptr())
+    torch.cuda.synchronize()
+    assert torch.equal(y, 2 * x) and torch.equal(q[:, 0].float(), 127 * torch.sign(x))

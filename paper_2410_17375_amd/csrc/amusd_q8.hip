@@ -397,8 +397,10 @@ hipError_t launch_q8_append(const amusd_q8_cache& c, int layer, const Q8Segs& S,
 // column).  2048 positions of 8 heads of 128 6 us, 5 of heads of 64 3.5.
 template <class T>
 __global__ void __launch_bounds__(256) k_q8_read(amusd_q8_cache C, int layer, Q8Segs S, T* __restrict__ kout, T* __restrict__ vout, int64_t ld) {
-    const Q8Seg& seg = q8_find(S, blockIdx.x);
-    const int p0 = (seg.pos0 / 4 + (int)blockIdx.x - seg.unit0) * 4, quads = C.Hkv * C.hd / 4;
+    const int unit = blockIdx.z * gridDim.x + blockIdx.x;
+    if (unit >= S.units) return;
+    const Q8Seg& seg = q8_find(S, unit);
+    const int p0 = (seg.pos0 / 4 + unit - seg.unit0) * 4, quads = C.Hkv * C.hd / 4;
     const bool values = blockIdx.y;
     T* out = (values ? vout : kout) + (int64_t)(seg.row0 - seg.pos0) * ld;
     for (int x = threadIdx.x; x < quads; x += blockDim.x) {
@@ -431,12 +433,13 @@ __global__ void __launch_bounds__(256) k_q8_read(amusd_q8_cache C, int layer, Q8
 
 hipError_t launch_q8_read(const amusd_q8_cache& c, int layer, const Q8Segs& segs, void* k, void* v, int dtype, int64_t ld, hipStream_t stream) {
     Q8Segs S = segs;
-    int units = 0;                                           // groups of 4 positions
+    S.units = 0;                                             // groups of 4 positions
     for (int i = 0; i < S.n_seg; ++i) {
-        S.s[i].unit0 = units;
-        units += (S.s[i].pos0 + S.s[i].n - 1) / 4 - S.s[i].pos0 / 4 + 1;
+        S.s[i].unit0 = S.units;
+        S.units += (S.s[i].pos0 + S.s[i].n - 1) / 4 - S.s[i].pos0 / 4 + 1;
     }
-    const dim3 grid(units, 2);
+    constexpr int kMost = 1 << 22;                           // (2^32 threads along one side of a grid and more are cut off without an error)
+    const dim3 grid(std::min(S.units, kMost), 2, (S.units + kMost - 1) / kMost);
     if (dtype == AMUSD_DTYPE_BF16)
         hipLaunchKernelGGL(k_q8_read<uint16_t>, grid, dim3(256), 0, stream, c, layer, S, static_cast<uint16_t*>(k), static_cast<uint16_t*>(v), ld);
     else

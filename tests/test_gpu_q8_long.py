@@ -114,3 +114,23 @@ def test_more_rows_than_a_launch_takes(gpu):
     A.q8_rmsnorm(x.data_ptr(), A.DTYPE_FP32, 1, x.data_ptr(), A.DTYPE_FP32, 1, gain.data_ptr(), 1e-5, rows, 1, y.data_ptr(), 1, q.data_ptr(), 16, s.data_ptr())
     torch.cuda.synchronize()
     assert torch.equal(y, 2 * x) and torch.equal(q[:, 0].float(), 127 * torch.sign(x))
+
+
+def test_read_of_2_26_positions(gpu):
+    """As many positions of several sequences at once as a launch of a workgroup for each four has no threads for."""
+    torch, A = gpu
+    capacity, seqs = 1 << 24, 5
+    cache = A.Q8Cache(n_layers=1, n_seqs=seqs, n_q_heads=1, n_kv_heads=1, head_dim=64, capacity=capacity, block=64)
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    n = (1 << 26) // seqs + 100
+    for i in range(seqs):
+        k, v = (torch.randn(100, 64, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+        cache.append(0, [i], [n - 100], [100], k.data_ptr(), v.data_ptr(), 64)
+    back = [torch.full((seqs * n, 64), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    cache.read(0, list(range(seqs)), [0] * seqs, [n] * seqs, back[0].data_ptr(), back[1].data_ptr(), A.DTYPE_BF16, 64)
+    one = [torch.empty(100, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for i in range(seqs):
+        cache.read(0, [i], [n - 100], [100], one[0].data_ptr(), one[1].data_ptr(), A.DTYPE_BF16, 64)
+        for a, b in zip(back, one):
+            assert b.any().item() and torch.equal(a[(i + 1) * n - 100:(i + 1) * n], b)
+            assert not a[i * n:(i + 1) * n - 200].any().item()          # (its last block of zeros ends there)

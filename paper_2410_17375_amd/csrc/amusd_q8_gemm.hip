@@ -381,9 +381,14 @@ static void gemm(const amusd_q8_matrix& w, const int8_t* x, int64_t ldx, const f
         using Sh = decltype(shape);
         const auto kernel = k_q8_gemm_tile<Sh, OUT, GATED>;
         (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Sh::kLds);
-        const int row_wgs = (rows + Sh::kRowTiles * 16 - 1) / (Sh::kRowTiles * 16), wgs = row_wgs * ((w.tiles + Sh::kColTiles - 1) / Sh::kColTiles);
-        hipLaunchKernelGGL(kernel, dim3(wgs, plan.ways), dim3(Sh::kThreads), Sh::kLds, stream, w.frag, w.scale, w.kblocks, w.k, w.tiles, w.n, x, ldx, scale,
-                           rows, out, ldo, row_wgs, wgs, work);
+        // (a launch of 2^32 threads and more is cut off without an error: at most 2^31, so many rows at a time)
+        const int col_wgs = (w.tiles + Sh::kColTiles - 1) / Sh::kColTiles;
+        const int64_t most = std::max(1, (1 << 22) / col_wgs) * (int64_t)(Sh::kRowTiles * 16);
+        for (int64_t r = 0; r < rows; r += most) {
+            const int n = (int)std::min(most, rows - r), row_wgs = (int)(((int64_t)n + Sh::kRowTiles * 16 - 1) / (Sh::kRowTiles * 16)), wgs = row_wgs * col_wgs;
+            hipLaunchKernelGGL(kernel, dim3(wgs, plan.ways), dim3(Sh::kThreads), Sh::kLds, stream, w.frag, w.scale, w.kblocks, w.k, w.tiles, w.n,
+                               x + r * ldx, ldx, scale + r, n, out + r * ldo, ldo, row_wgs, wgs, work);
+        }
     };
     switch (plan.form) {
         case kQ8Few1x1: if constexpr (!GATED) return few(k_q8_gemm_rows<OUT, GATED, 1, 1, 4>, 1, 1); else return;

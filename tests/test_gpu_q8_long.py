@@ -134,3 +134,23 @@ def test_read_of_2_26_positions(gpu):
         for a, b in zip(back, one):
             assert b.any().item() and torch.equal(a[(i + 1) * n - 100:(i + 1) * n], b)
             assert not a[i * n:(i + 1) * n - 200].any().item()          # (its last block of zeros ends there)
+
+
+@pytest.mark.parametrize("n,gated,dtype", [(1, False, "bfloat16"), (4, True, "bfloat16")])
+def test_product_of_2_30_rows(gpu, n, gated, dtype):
+    torch, A = gpu
+    rows, k = (1 << 30) + 77, 16
+    w = (np.arange(n * k).reshape(n, k) % 7 - 3).astype(np.int8)
+    w[:, 0] = 5 + np.arange(n)
+    m = A.Q8Matrix(w, A.DTYPE_INT8, n, k, scale=np.full(n, 0.5, np.float32), gated=gated)
+    x = torch.zeros(rows, k, dtype=torch.int8, device="cuda")
+    pattern = (torch.arange(1000, device="cuda") % 250 - 125).to(torch.int8)
+    x[:, 0] = pattern.repeat(rows // 1000 + 1)[:rows]
+    s = torch.ones(rows, device="cuda")
+    cols = n // 2 if gated else n
+    out, few = torch.full((rows, cols), 99.0, dtype=torch.bfloat16, device="cuda"), torch.empty(1000, cols, dtype=torch.bfloat16, device="cuda")
+    A.q8_gemm(m, x.data_ptr(), k, s.data_ptr(), 1000, few.data_ptr(), A.DTYPE_BF16, cols)
+    A.q8_gemm(m, x.data_ptr(), k, s.data_ptr(), rows, out.data_ptr(), A.DTYPE_BF16, cols)
+    torch.cuda.synchronize()
+    whole = rows // 1000 * 1000
+    assert (out[:whole].view(-1, 1000, cols) == few).all().item() and torch.equal(out[whole:], few[:rows - whole])

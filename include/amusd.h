@@ -311,7 +311,7 @@ int amusd_q8_rmsnorm(const void *x, int32_t dtype, int64_t ldx, const void *add,
  * w: row-major [n][ld], fp32 or bf16 (rounded to 8 bits here; scale is NULL), or 8-bit integers in [-127, 127] with
  * their scales; host (on_device = 0) or device memory, not referenced after the call.  gated: the first n/2 features are the
  * gate's and the others the up projection's of a SwiGLU, and the product gives silu(gate) * up, n/2 columns.
- * k is at most 131072 (sums stay inside 32 bits). */
+ * k is at most 131072 (sums stay inside 32 bits), n below 2^28. */
 typedef struct amusd_q8_matrix amusd_q8_matrix;
 int amusd_q8_matrix_create(const void *w, int32_t dtype, const float *scale, int32_t n, int32_t k, int64_t ld,
                            int32_t gated, int32_t on_device, void *hip_stream, amusd_q8_matrix **out);

@@ -449,12 +449,12 @@ hipError_t launch_q8_read(const amusd_q8_cache& c, int layer, const Q8Segs& segs
 
 // ---------------------------------------------------------------- weights to 8 bits, in operand order
 // One wave a row of the source: finds its scale (unless it is given), then writes the feature's bytes.  Row i is feature first + i
-// of the matrix or, in a gated one, its gate's or up projection's (part 1, 2) feature i.
+// of the matrix or, in a gated one, of its gate or up projection (part 1, 2).
 template <class T>
 __global__ void __launch_bounds__(64) k_q8_matrix(uint4* __restrict__ frag, float* __restrict__ scale, const T* __restrict__ w, int64_t ld,
                                                   const float* __restrict__ given, int k, int first, int part) {
-    const int i = blockIdx.x, lane = threadIdx.x;
-    const int tile = part ? (i >> 4) * 2 + part - 1 : (first + i) >> 4, r = part ? i & 15 : (first + i) & 15;
+    const int i = blockIdx.x, f = first + i, lane = threadIdx.x;
+    const int tile = part ? (f >> 4) * 2 + part - 1 : f >> 4, r = f & 15;
     w += i * ld;
     float s = 0.f, inv = 0.f;
     auto value = [&](int c) {
@@ -485,7 +485,10 @@ __global__ void __launch_bounds__(64) k_q8_matrix(uint4* __restrict__ frag, floa
 hipError_t launch_q8_matrix(const amusd_q8_matrix& m, const void* w, int dtype, int64_t ld, const float* scale, int rows, int first, int part,
                             hipStream_t stream) {
     auto go = [&](auto kernel, auto* src) {
-        hipLaunchKernelGGL(kernel, dim3(rows), dim3(64), 0, stream, const_cast<uint4*>(m.frag), const_cast<float*>(m.scale), src, ld, scale, m.k, first, part);
+        constexpr int kMost = 1 << 25;                       // (2^32 threads and more are cut off without an error)
+        for (int r = 0; r < rows; r += kMost)
+            hipLaunchKernelGGL(kernel, dim3(std::min(kMost, rows - r)), dim3(64), 0, stream, const_cast<uint4*>(m.frag), const_cast<float*>(m.scale),
+                               src + r * ld, ld, scale ? scale + r : nullptr, m.k, first + r, part);
     };
     if (dtype == AMUSD_DTYPE_FP32) go(k_q8_matrix<uint32_t>, static_cast<const uint32_t*>(w));
     else if (dtype == AMUSD_DTYPE_BF16) go(k_q8_matrix<uint16_t>, static_cast<const uint16_t*>(w));
@@ -664,7 +667,7 @@ int amusd_q8_matrix_create(const void* w, int32_t dtype, const float* scale, int
     if (!w || !out) return report(AMUSD_E_ARG, "q8_matrix: null argument");
     if (!float_dtype(dtype) && dtype != AMUSD_DTYPE_INT8) return report(AMUSD_E_ARG, "q8_matrix: unknown dtype");
     if ((dtype == AMUSD_DTYPE_INT8) != (scale != nullptr)) return report(AMUSD_E_ARG, "q8_matrix: scales go with 8-bit weights, and only with them");
-    if (n < 1 || k < 1 || ld < k || (gated && n % 2) || n > (1 << 28) || k > kQ8MaxK) return report(AMUSD_E_ARG, "q8_matrix: bad sizes");
+    if (n < 1 || k < 1 || ld < k || (gated && n % 2) || n >= (1 << 28) || k > kQ8MaxK) return report(AMUSD_E_ARG, "q8_matrix: bad sizes");
     amusd_q8_matrix* m = new (std::nothrow) amusd_q8_matrix();
     if (!m) return report(AMUSD_E_NOMEM, "q8_matrix: handle");
     const size_t esz = dtype == AMUSD_DTYPE_FP32 ? 4 : dtype == AMUSD_DTYPE_BF16 ? 2 : 1;

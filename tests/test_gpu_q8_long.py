@@ -154,3 +154,16 @@ def test_product_of_2_30_rows(gpu, n, gated, dtype):
     torch.cuda.synchronize()
     whole = rows // 1000 * 1000
     assert (out[:whole].view(-1, 1000, cols) == few).all().item() and torch.equal(out[whole:], few[:rows - whole])
+
+
+def test_matrix_of_2_26_features(gpu):
+    """A wave rounds a feature: more features than a launch has waves."""
+    torch, A = gpu
+    n = (1 << 26) + 53
+    w = torch.arange(n, dtype=torch.int32, device="cuda").remainder_(1013).float() - 500
+    torch.cuda.synchronize()
+    m = A.Q8Matrix(w.data_ptr(), A.DTYPE_FP32, n, 1, on_device=True)
+    x, s = torch.ones(1, 16, dtype=torch.int8, device="cuda"), torch.ones(1, device="cuda")
+    out = torch.empty(n, device="cuda")
+    A.q8_gemm(m, x.data_ptr(), 16, s.data_ptr(), 1, out.data_ptr(), A.DTYPE_FP32, n)
+    assert torch.equal(out, 127 * (torch.abs(w) / torch.full_like(w, 127)) * torch.sign(w))

@@ -62,6 +62,12 @@ def test_matrix_and_product(L):
     assert L.amusd_q8_gemm(None, P, 64, P, 1, P, 0, 4, None, 0, None) == -1
 
 
+def test_matrix_of_more_features_than_a_launch(L):
+    h = C.c_void_p()
+    _refused(L.amusd_q8_matrix_create(P, 0, None, 1 << 28, 1, 1, 0, 1, None, C.byref(h)), L)      # two tiles a workgroup of 512: 2^32 threads
+    assert not h
+
+
 def test_matrix_of_a_host_array(L):
     """The binding hands over no array that is shorter than what the call reads, nor one whose rows lie otherwise."""
     import paper_2410_17375_amd as A

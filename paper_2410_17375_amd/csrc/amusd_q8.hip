@@ -528,6 +528,11 @@ void q8_matrix_drop(amusd_q8_matrix& m) {
     m.scale = nullptr;
 }
 
+// (in floating point: the product need not fit 64 bits)
+static double q8_cache_bytes(int n_layers, int n_seqs, int n_kv_heads, int head_dim, int capacity) {
+    return 2. * n_layers * n_seqs * n_kv_heads * head_dim * capacity;
+}
+
 hipError_t q8_cache_take(amusd_q8_cache& c, int n_layers, int n_seqs, int n_q_heads, int n_kv_heads, int head_dim, int capacity, int block, Q8Alloc alloc,
                          hipStream_t stream) {
     c.n_layers = n_layers;
@@ -538,6 +543,7 @@ hipError_t q8_cache_take(amusd_q8_cache& c, int n_layers, int n_seqs, int n_q_he
     c.G = n_q_heads / n_kv_heads;
     c.block = block;
     c.cap = (capacity + kQ8Group - 1) / kQ8Group * kQ8Group;
+    if (q8_cache_bytes(n_layers, n_seqs, n_kv_heads, head_dim, capacity) > kQ8MaxBytes) return hipErrorOutOfMemory;
     hipError_t e = q8_device(c.device, c.cus);
     q8_attention_plan(c);
     const size_t heads = (size_t)n_layers * n_seqs * n_kv_heads, bytes = heads * c.cap * head_dim, scales = heads * (c.cap / block) * 4;
@@ -667,7 +673,8 @@ int amusd_q8_matrix_create(const void* w, int32_t dtype, const float* scale, int
     if (!w || !out) return report(AMUSD_E_ARG, "q8_matrix: null argument");
     if (!float_dtype(dtype) && dtype != AMUSD_DTYPE_INT8) return report(AMUSD_E_ARG, "q8_matrix: unknown dtype");
     if ((dtype == AMUSD_DTYPE_INT8) != (scale != nullptr)) return report(AMUSD_E_ARG, "q8_matrix: scales go with 8-bit weights, and only with them");
-    if (n < 1 || k < 1 || ld < k || (gated && n % 2) || n >= (1 << 28) || k > kQ8MaxK) return report(AMUSD_E_ARG, "q8_matrix: bad sizes");
+    if (n < 1 || k < 1 || ld < k || (gated && n % 2) || n >= (1 << 28) || k > kQ8MaxK || (double)(n - 1) * (double)ld > kQ8MaxBytes)
+        return report(AMUSD_E_ARG, "q8_matrix: bad sizes");
     amusd_q8_matrix* m = new (std::nothrow) amusd_q8_matrix();
     if (!m) return report(AMUSD_E_NOMEM, "q8_matrix: handle");
     const size_t esz = dtype == AMUSD_DTYPE_FP32 ? 4 : dtype == AMUSD_DTYPE_BF16 ? 2 : 1;
@@ -729,7 +736,7 @@ int amusd_q8_cache_create(int32_t n_layers, int32_t n_seqs, int32_t n_q_heads, i
                           void* hip_stream, amusd_q8_cache** out) {
     if (!out) return report(AMUSD_E_ARG, "q8_cache: null argument");
     if (n_layers < 1 || n_seqs < 1 || n_seqs > AMUSD_MAX_SEQS || n_q_heads < 1 || n_kv_heads < 1 || n_kv_heads > 65535 || capacity < 1 ||
-        capacity > kQ8MaxPositions)
+        capacity > kQ8MaxPositions || q8_cache_bytes(n_layers, n_seqs, n_kv_heads, head_dim, capacity) > kQ8MaxBytes)
         return report(AMUSD_E_ARG, "q8_cache: bad sizes");
     if (head_dim != 64 && head_dim != 128) return report(AMUSD_E_ARG, "q8_cache: head_dim must be 64 or 128");
     if (block != 1 && block != 16 && block != 32 && block != 64) return report(AMUSD_E_ARG, "q8_cache: block must be 1, 16, 32 or 64");

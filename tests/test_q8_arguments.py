@@ -62,6 +62,18 @@ def test_matrix_and_product(L):
     assert L.amusd_q8_gemm(None, P, 64, P, 1, P, 0, 4, None, 0, None) == -1
 
 
+def test_sizes_past_64_bits(L):
+    """Products of sizes, each of which is allowed, that do not fit the type of an allocation's size."""
+    h = C.c_void_p()
+    for layers, seqs, heads, capacity in ((1 << 30, 4096, 2, 1 << 24), (1 << 20, 4096, 1 << 13, 1 << 24), (2 ** 31 - 1, 4096, 65535, 1 << 24), (1 << 17, 4096, 4096, 1 << 23)):
+        _refused(L.amusd_q8_cache_create(layers, seqs, heads, heads, 128, capacity, 1, None, C.byref(h)), L)
+        assert not h
+    for on_device in (0, 1):
+        for n, ld in ((1 << 20, 1 << 44), (3, 1 << 62), (2, 2 ** 63 - 1)):
+            _refused(L.amusd_q8_matrix_create(P, 0, None, n, 64, ld, 0, on_device, None, C.byref(h)), L)
+            assert not h
+
+
 def test_matrix_of_more_features_than_a_launch(L):
     h = C.c_void_p()
     _refused(L.amusd_q8_matrix_create(P, 0, None, 1 << 28, 1, 1, 0, 1, None, C.byref(h)), L)      # two tiles a workgroup of 512: 2^32 threads

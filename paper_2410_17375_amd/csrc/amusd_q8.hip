@@ -206,9 +206,12 @@ template <class X, class A, bool NORM>
 static void q8_rows(const void* x, int64_t ldx, const void* add, int64_t ldadd, const float* gain, float eps, int rows, int n, void* sum, int64_t ldsum,
                     int8_t* q, int64_t ldq, float* scale, hipStream_t stream) {
     // Vectors of 8 elements a thread, where only the largest is sought: one for few rows, as then the way through one row counts (8 x 14336 5.8 us for
-    // 6.2); four for many and long ones, for more workgroups a compute unit, in different phases (2048 x 14336 22.8 us for 25.4; 2048 x 4096 and
-    // x 8192 10.4 for 9.4 and 15.9 for 15.3).  A norm has two whatever the number of rows: its sum of squares has its order from that.
-    const int vectors = NORM ? 2 : rows <= 128 ? 1 : rows > 1024 && n > 8 * 1024 ? 4 : 2;
+    // 6.2); four for many long ones in bf16, for more workgroups a compute unit, in different phases.  us with four / two, inputs from memory: 2048 x
+    // 10240 21.2 / 22.5, x 12288 24.7 / 24.3, x 14336 26.1 / 29.7, 4096 x 6144 22.6 / 23.5, x 8192 28.0 / 28.3, 8192 x 16384 89 / 101; below either bound
+    // 4096 x 4096 17.1 / 15.8, 1100 x 8208 13.4 / 12.3, 2048 x 9216 19.7 / 19.0; fp32 2048 x 10240 23.7 / 23.6, 4096 x 14336 56.6 / 55.4,
+    // 8192 x 16384 125 / 118.  A norm has two whatever the number of rows: its sum of squares has its order from that.
+    const bool many_long = sizeof(X) == 2 && n >= 6144 && (int64_t)rows * n >= 20 << 20;
+    const int vectors = NORM ? 2 : rows <= 128 ? 1 : many_long ? 4 : 2;
     const int threads = (int)std::min<int64_t>(1024, ((int64_t)n + vectors * 512 - 1) / (vectors * 512) * 64);
     // (a launch of 2^32 threads and more ends without an error and without its last workgroups)
     const int most = (int)(0xFFFFFFFFu / threads);

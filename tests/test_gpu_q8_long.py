@@ -167,3 +167,19 @@ def test_matrix_of_2_26_features(gpu):
     out = torch.empty(n, device="cuda")
     A.q8_gemm(m, x.data_ptr(), 16, s.data_ptr(), 1, out.data_ptr(), A.DTYPE_FP32, n)
     assert torch.equal(out, 127 * (torch.abs(w) / torch.full_like(w, 127)) * torch.sign(w))
+
+
+@pytest.mark.parametrize("rows,n", [(2048, 10240), (2100, 10300), (4000, 6144), (1700, 14336), (700, 32000), (700, 32768), (700, 32769)])
+def test_quantize_many_long_rows_as_few(gpu, rows, n):
+    """bf16 rows are laid over threads otherwise where they are many and long: on either side of that, and of what registers hold."""
+    torch, A = gpu
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.randn(rows, n, generator=gen, device="cuda").to(torch.bfloat16)
+    ld, got = -(-n // 16) * 16, []
+    for step in (rows, 90):
+        q, s = torch.zeros((rows, ld), dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+        for r in range(0, rows, step):
+            A.q8_quantize(x[r].data_ptr(), A.DTYPE_BF16, n, min(step, rows - r), n, q[r].data_ptr(), ld, s[r:].data_ptr())
+        got.append((q, s))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    assert (got[0][0].abs().amax(1) == 127).all().item()

@@ -14,8 +14,16 @@ __device__ __forceinline__ v4i mfma_i8(uint4 a, uint4 b, v4i c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, a), __builtin_bit_cast(v4i, b), c, 0, 0, 0);
 }
 
-// What every form of the product makes of a sum, in this order: a row's bits do not depend on the form.
-__device__ __forceinline__ float q8_value(int sum, float sx, float sw) { return (float)sum * sx * sw; }
+// What every form of the product makes of a sum, in this order: a row's bits do not depend on the form.  A large row scale (rows of 1e21 and more) is
+// taken down by a power of two, which the result is given back: the sum times it could be past float32 where the result is not.
+struct Q8RowScale {
+    float s, back;
+};
+__device__ __forceinline__ Q8RowScale q8_row_scale(float s) {
+    const bool large = s >= 0x1p64f;
+    return {large ? s * 0x1p-40f : s, large ? 0x1p40f : 1.f};
+}
+__device__ __forceinline__ float q8_value(int sum, Q8RowScale sx, float sw) { return (float)sum * sx.s * sw * sx.back; }
 __device__ __forceinline__ void q8_put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void q8_put(uint16_t* p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
 // silu(gate) * up.  With the instructions for 2^x and 1/x (an error of one unit in the last place each): a division in full is ten
@@ -130,7 +138,7 @@ __global__ void __launch_bounds__(512) k_q8_gemm_rows(const uint4* __restrict__ 
         const int t = f >> 4, m = row >> 4, at = (row & 15) * 16 + (f & 15);
         const int gr = row0 + row, gc = (GATED ? tile0 / 2 : tile0) * 16 + f;
         if (gr >= rows || gc >= n) continue;
-        const float sx = xscale[gr];
+        const Q8RowScale sx = q8_row_scale(xscale[gr]);
         float v;
         if constexpr (GATED) {
             const float* s = wscale + (tile0 + 2 * t) * 16 + (f & 15);
@@ -334,7 +342,7 @@ __global__ void __launch_bounds__(Sh::kThreads, Sh::kMinWaves) k_q8_gemm_tile(co
 #pragma unroll
     for (int j = 0; j < B; ++j) {
         const int jrow = row0 + (wm * B + j) * 16;
-        const float sx = xscale[min(jrow + r, rows - 1)];
+        const Q8RowScale sx = q8_row_scale(xscale[min(jrow + r, rows - 1)]);
 #pragma unroll
         for (int i = 0; i < A; i += GATED ? 2 : 1) {
             OUT v[4];

@@ -281,3 +281,41 @@ def test_attention_of_a_far_largest_score(gpu, heads, n, rows):
     # one weight: its value's half step in bf16; the weight times its value's scale to half (2^-11), where the denominator has the weight as
     # it is; and the step that the chain of fp32 sums with 1152 + v leaves
     assert (np.abs(got - want) <= (U16 + 1.01 * 2.0 ** -11) * np.abs(want) + 4 * U32 * 1280 / 127 * np.abs(v).max()).all()
+
+
+# ---------------------------------------------------------------- products of rows with large scales
+@pytest.mark.parametrize("rows,n,k", [(1, 100, 600), (8, 512, 4096), (40, 300, 1000), (200, 512, 2048), (600, 1040, 640)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_gemm_of_large_row_scales(gpu, rows, n, k, gated):
+    """The sum times the row's scale is past float32, the result is not: rows of magnitudes around 1e34, weights around 1e-4."""
+    torch, A = gpu
+    rng = np.random.default_rng([rows, n, k])
+    w = rng.integers(-127, 128, (n, k)).astype(np.int8)
+    w[:, 0] = 127
+    sw = ((rng.random(n) + 0.5) * 1e-6).astype(np.float32)
+    if gated:
+        sw[n // 2:] *= np.float32(1e-28)                      # (both halves are large otherwise)
+    x = rng.integers(100, 128, (rows, k)).astype(np.int8)
+    x[:, 1::2] *= -1
+    sx = (2.0 ** rng.uniform(60, 121, rows)).astype(np.float32)
+    sx[0] = 2.0 ** 115
+    sx[1::3] = (rng.random(len(sx[1::3])) + 0.5) * 0.01      # ordinary ones beside them
+    m = A.Q8Matrix(w, A.DTYPE_INT8, n, k, scale=sw, gated=gated)
+    y = O.gemm(x, sx, w, sw)
+    got = _np(_product(gpu, m, x, sx, n // 2 if gated else n, torch.float32))
+    if not gated:
+        fine = np.abs(y) < 3.3e38
+        assert (np.abs(got - y) <= 3.01 * U32 * np.abs(y))[fine].all()
+        assert fine.mean() > 0.9 and (np.abs(y) > 1e30).any()
+        alone = _np(_product(gpu, m, x, sx, n, torch.float32, work=False))
+        assert np.array_equal(got, alone)
+        for r in (0, rows - 1):
+            assert np.array_equal(_np(_product(gpu, m, x[r:r + 1], sx[r:r + 1], n, torch.float32))[0], got[r])
+        return
+    gate = y[:, :n // 2]
+    with np.errstate(over="ignore"):
+        want = np.where(gate < -700, 0, O.swiglu(y))
+    # beyond a score of units silu is the gate itself or 0; errors as in test_gpu_q8.py, where the exponential's are within a unit's range
+    sure = (np.abs(want) < 3.3e38) & ((gate > 100) | (gate < -200))
+    assert sure.any()
+    assert (np.abs(got - want) <= 9 * U32 * np.abs(want) + 1e-37)[sure].all()

@@ -13,13 +13,14 @@
 namespace amusd {
 
 // ---------------------------------------------------------------- rows to 8 bits
-// A workgroup a row, the row in registers: it is read once and written once, so the bytes bound it (and its launch, where
-// there are few rows).  Loads and stores take any alignment (one instruction of 16 bytes all the same).  Sums of squares, their root and the normalised
+// A workgroup a row, the row in registers: it is read once and written once.  Bound by its launch where there are few rows; with many by the
+// way through a row, whose loads, reduction and stores come one after the other: waves wait 58 to 68 % of their cycles, vector instructions
+// take 72 % of those in which a compute unit is busy (2048 x 14336: 19 an element) or 32 % (1531 x 2055 with norm).  Loads and stores take any alignment (one instruction of 16 bytes all the same).  Sums of squares, their root and the normalised
 // element are in 64 bits, the element then rounded to 32: a square of a large element stays finite.
 // The quotient is taken as the product with the scale's reciprocal, and divided in full only where that is too near the middle between
 // two integers to tell (half the largest value stands on one); adding 1.5 * 2^23 leaves the nearest integer, ties to even, in the low bits.
-// Measured (MI355X): 2048 x 14336 bf16 23-26 us (3.4-3.9 TB/s; a division for each element 53), 2048 x 4096 fp32 + bf16 with norm and sum 25 (3.7 TB/s),
-// 1531 x 2055 14.5 (rows of odd length), 8 x 4096 with norm 5.7, 1 x 2048 2.5.
+// Measured (MI355X): 2048 x 14336 bf16 26 us (3.4 TB/s; a division for each element 53), 2048 x 4096 fp32 + bf16 with norm and sum 25 (3.7 TB/s),
+// 1531 x 2055 14.5-15 (a third of its vectors of 8 are empty), 8 x 4096 with norm 5.8, 1 x 2048 2.3.
 template <class T>
 __device__ __forceinline__ void q8_load(const T* p, int n, float (&v)[8]) {       // n: elements there are, 1 or more
     T e[8];
@@ -248,8 +249,9 @@ hipError_t launch_q8_rows(const void* x, int dtype, int64_t ldx, const void* add
 // A workgroup owns 64 positions of one kv head's keys or values (blocks do not reach over that), so nothing is shared between
 // workgroups.  16 lanes hold a row (its rotary pairs in one lane), so its largest element needs four lane exchanges; the rows then
 // lie in LDS for the store in the cache's order.  Blocks that held tokens before keep their scale unless a new value outgrows it;
-// then what they hold is rounded once more, to the new scale.  Bound by its passes through LDS and the order of the stores: 2048 rows of 8 heads
-// of 128 in blocks of 32 12-13 us (1.0 TB/s), 5 rows of 8 heads of 64 4.6.
+// then what they hold is rounded once more, to the new scale.  Bound by its phases, one after the other between barriers, of eight waves a compute
+// unit (they wait 49 % of their cycles; vector instructions take 30 % of the busy ones) with stores of 4 bytes at a distance of 16 for
+// values: 2048 rows of 8 heads of 128 in blocks of 32 12-13 us (1.0 TB/s), 5 rows of 8 heads of 64 4.8.
 __device__ __forceinline__ const Q8Seg& q8_find(const Q8Segs& S, int unit) {
     int i = 0;
     while (i + 1 < S.n_seg && unit >= S.s[i + 1].unit0) ++i;

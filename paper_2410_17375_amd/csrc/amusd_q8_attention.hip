@@ -5,16 +5,18 @@
 // half as many matrix instructions as half precision would take, and no key is converted.  The rounding of a query moves a score
 // by at most 2^-16 of (its largest component times the sum of the key's magnitudes).  Softmax weights carry the scales of their
 // values, are brought below 2^15 by a power of two and rounded to half (11 bits); values are exact in half.  Maxima, sums and
-// results are fp32.
+// results are fp32.  One half a weight, where two would take twice the products of weights and values: the result is rounded to bf16, an
+// eighth as fine, and lies as far from 64 bits as one whose weights are fp32 (0.0017 to 0.0018 of its norm for 0.0016 to 0.0017).
 //
 // Keys are taken in chunks at absolute positions, whose sums start anew and are merged in order, whoever does it: with few rows a
 // wave takes one chunk and a second launch merges (k_q8_att_part, k_q8_att_merge), with many a wave walks all of them
 // (k_q8_att_whole).  What a chunk's sums depend on is only what the row may see.  So a row's bits depend neither on how many
-// rows a call has nor on the form.
+// rows a call has nor on the form; they do on the chunks (q8_attention_plan).
 //
-// Bound by the instructions between the two products (81 % of the issue slots of a SIMD are vector instructions': scales, 2^x, maxima,
-// roundings, bytes to halves).  Measured (MI355X; part + merge, or whole), 8B heads: 16 rows behind 16384 keys 20 + 8 us (34 MB of cache),
-// 8 rows behind 2048 12 in all, 1111 rows behind 1024 in blocks of 64 84, 2048 rows of a prompt 84; 1B heads: 1 row behind 512 5 + 4.
+// Bound by the instructions between the two products (vector instructions take 76 to 96 % of the cycles in which a compute unit is busy: scales,
+// 2^x, maxima, roundings, bytes to halves).  Measured (MI355X; part + merge, or whole), 8B heads: 16 rows behind 16384 keys 22 + 8 us (34 MB of cache),
+// 8 rows behind 2048 13 in all, 1111 rows behind 1024 in blocks of 64 87 after a pause, 77 in a long run of them (the clock rises), 2048 rows of
+// a prompt 84-86; 1B heads: 1 row behind 512 5.6 + 4.
 #include <algorithm>
 
 #include "amusd_math.h"

@@ -26,8 +26,8 @@ __device__ __forceinline__ Q8RowScale q8_row_scale(float s) {
 __device__ __forceinline__ float q8_value(int sum, Q8RowScale sx, float sw) { return (float)sum * sx.s * sw * sx.back; }
 __device__ __forceinline__ void q8_put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void q8_put(uint16_t* p, float v) { *p = __builtin_bit_cast(uint16_t, (__bf16)v); }
-// silu(gate) * up.  With the instructions for 2^x and 1/x (an error of one unit in the last place each): a division in full is ten
-// instructions more for each of the outputs, which wait for nothing else.
+// silu(gate) * up.  With the instructions for 2^x and 1/x (an error of one unit in the last place each; the rounding of 2^x's argument adds |gate|
+// half units): a division in full is ten instructions more for each of the outputs, which wait for nothing else.
 __device__ __forceinline__ float q8_swiglu(float gate, float up) {
     return gate * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(gate * -1.44269504f)) * up;
 }
@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(512) k_q8_gemm_rows(const uint4* __restrict__ 
 //   rows two blocks at a time (3 slots), a load fetching 8 whole lines of 128 bytes: with 16 half lines a load, a block of 256 x 256 took
 //   0.75 us instead of 0.56.  The eight 16-byte pieces of a line lie in an order that depends on the row, so that the 16
 //   lanes that read a column of pieces find them in different banks.
-// Measured (MI355X), 2048 rows: 28672 x 4096 gated 208-217 us (2.2-2.3 POP/s; with every compute unit multiplying a block of 256 x 256 takes 0.70
+// Measured (MI355X), 2048 rows: 28672 x 4096 gated 208-217 us, 230 after a pause (2.2-2.3 POP/s; with every compute unit multiplying a block of 256 x 256 takes 0.70
 // us, at the clock that their power leaves), 6144 x 4096 53, 4096 x 4096 38, 4096 x 14336 118-124; 8192 x 8192 of 8192 rows 2.47 POP/s.
 template <int WN_, int WM_, int A_, int B_, int WAVES_>
 struct Q8Shape {

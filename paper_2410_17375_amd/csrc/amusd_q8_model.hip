@@ -88,8 +88,6 @@ __global__ void __launch_bounds__(1024) k_q8_greedy(const float* __restrict__ lo
 }
 __global__ void __launch_bounds__(256) k_q8_export(DevModel M, int bytes) { export_logits(M, bytes, blockIdx.x); }
 
-constexpr int kLmRows = 256;       // rows of a prompt whose logits are there at a time (a prompt of 2048 through 4 layers and 128256 tokens: 4.07 ms; 128 rows: 4.78)
-
 struct Stage {                     // events around the launches of the stage that is timed
     StageTimer* tm;
     hipStream_t stream;
@@ -230,7 +228,7 @@ size_t q8_model_bufs(const Q8Model* q, const DevModel& D, int cap, uintptr_t bas
     for (const amusd_q8_matrix* m : {&q->layers[0].qkv, &q->layers[0].o, &q->layers[0].gu, &q->layers[0].down, &q->lm})
         B.work_bytes = std::max(B.work_bytes, q8_gemm_workspace(*m, cap));
     B.work = place(B.work_bytes);
-    B.logits = static_cast<float*>(place(cap > kRows ? (size_t)std::min(cap, kLmRows) * D.V * 4 : 0));
+    B.logits = static_cast<float*>(place(cap > kRows ? (size_t)std::min(cap, kQ8LmRows) * D.V * 4 : 0));
     return off;
 }
 
@@ -267,7 +265,7 @@ hipError_t q8_model_prefill(const Q8Model* Q, const DevModel& D, const DevLayer*
     TRY(layers_of(*Q, D, Ls, B, S, tokens, s, Stage{nullptr, s}));
     // The last `tail` rows' logits can be asked for; of the others only the arg-max is kept.
     for (int r = 0; r < P.n;) {
-        const int rows = r < P.n - tail ? std::min(P.n - tail - r, kLmRows) : tail;
+        const int rows = r < P.n - tail ? std::min(P.n - tail - r, kQ8LmRows) : tail;
         float* z = r < P.n - tail ? B.logits : D.logits;
         TRY(launch_q8_gemm(Q->lm, B.q + (size_t)r * D.d, D.d, B.s + r, rows, z, AMUSD_DTYPE_FP32, D.V, B.work, B.work_bytes, s));
         hipLaunchKernelGGL(k_q8_greedy, dim3(rows), dim3(1024), 0, s, z, D.V, T.greedy + r);

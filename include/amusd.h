@@ -58,7 +58,7 @@ extern "C" {
                                   * below one after the other.  It is another model than the bf16 one of the same tensors, and keeps
                                   * the same promises: exact loops, rows whose bits depend on their sequence alone (among models of
                                   * one max_ctx: attention's chunks follow from it, amusd_q8_attention).  Widths are at
-                                  * most 131072, max_ctx 2^24 (else ARG) */
+                                  * most 131072, max_ctx 2^24, the vocabulary below 2^28 (else ARG) */
 #define AMUSD_MAX_K        16   /* rows of one pass: the 16-row matrix-core tile */
 #define AMUSD_MAX_SEQS   4096   /* sequences (key-value caches) one model can hold */
 

@@ -211,8 +211,8 @@ int check_config(const amusd_config* c) {
     const long qdim = (long)c->n_q_heads * c->head_dim;
     if (c->d_model % kb || qdim % kb || c->d_ffn % kb)
         return fail(AMUSD_E_ARG, "config: d_model, n_q_heads*head_dim and d_ffn must be multiples of the fragment width");
-    if (c->dtype == AMUSD_DTYPE_INT8 && (c->d_model > kQ8MaxK || qdim > kQ8MaxK || c->d_ffn > kQ8MaxK || c->max_ctx > kQ8MaxPositions))
-        return fail(AMUSD_E_ARG, "config: an 8-bit model's widths are at most 131072, its context 2^24");
+    if (c->dtype == AMUSD_DTYPE_INT8 && (c->d_model > kQ8MaxK || qdim > kQ8MaxK || c->d_ffn > kQ8MaxK || c->max_ctx > kQ8MaxPositions || c->vocab >= kQ8MaxFeatures))
+        return fail(AMUSD_E_ARG, "config: an 8-bit model's widths are at most 131072, its context 2^24, its vocabulary below 2^28");
     if (c->d_model % 16 || c->d_ffn % 16 || c->vocab % 16)
         return fail(AMUSD_E_ARG, "config: d_model, d_ffn and vocab must be multiples of 16");
     if (!(c->rope_theta > 0.f) || !(c->rms_eps >= 0.f)) return fail(AMUSD_E_ARG, "config: rope_theta/rms_eps");

@@ -38,6 +38,7 @@ namespace amusd {
 int report(int code, const char* what, const char* detail = nullptr);
 
 constexpr int kQ8MaxK = 1 << 17;     // columns of a contraction: its sum of products of 127 * 127 stays inside 32 bits
+constexpr int kQ8MaxFeatures = 1 << 28;      // of a matrix (fewer): two tiles of 16 a workgroup of 512 are then fewer than 2^32 threads
 constexpr int kQ8MaxPositions = 1 << 24;     // of a sequence: chunks of 512 keys are a grid's third side
 constexpr double kQ8MaxBytes = 0x1p48;     // of an allocation: sizes that come to more are refused before their product is taken in 64 bits
 constexpr int kQ8MaxRow = 2 * 8 * 1024;   // columns of a row that a workgroup keeps in registers

@@ -678,7 +678,7 @@ int amusd_q8_matrix_create(const void* w, int32_t dtype, const float* scale, int
     if (!w || !out) return report(AMUSD_E_ARG, "q8_matrix: null argument");
     if (!float_dtype(dtype) && dtype != AMUSD_DTYPE_INT8) return report(AMUSD_E_ARG, "q8_matrix: unknown dtype");
     if ((dtype == AMUSD_DTYPE_INT8) != (scale != nullptr)) return report(AMUSD_E_ARG, "q8_matrix: scales go with 8-bit weights, and only with them");
-    if (n < 1 || k < 1 || ld < k || (gated && n % 2) || n >= (1 << 28) || k > kQ8MaxK || (double)(n - 1) * (double)ld > kQ8MaxBytes)
+    if (n < 1 || k < 1 || ld < k || (gated && n % 2) || n >= kQ8MaxFeatures || k > kQ8MaxK || (double)(n - 1) * (double)ld > kQ8MaxBytes)
         return report(AMUSD_E_ARG, "q8_matrix: bad sizes");
     amusd_q8_matrix* m = new (std::nothrow) amusd_q8_matrix();
     if (!m) return report(AMUSD_E_NOMEM, "q8_matrix: handle");

@@ -125,6 +125,15 @@ def test_models(L):
         assert not h
 
 
+def test_model_of_a_vocabulary_that_no_product_takes(L):
+    import paper_2410_17375_amd as A
+    cfg = A.Config(*dict(n_layers=1, d_model=64, n_q_heads=1, n_kv_heads=1, head_dim=64, d_ffn=64, vocab=1 << 28, max_ctx=64, max_k=8, dtype=A.DTYPE_INT8,
+                         rope_theta=1e4, rms_eps=1e-5, max_seqs=1).values())
+    h = C.c_void_p()
+    _refused(L.amusd_model_create(C.byref(cfg), None, C.byref(h)), L)
+    assert not h
+
+
 def test_calls_need_a_device(L):
     torch = pytest.importorskip("torch")
     if torch.cuda.is_available():

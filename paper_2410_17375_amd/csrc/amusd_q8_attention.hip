@@ -292,7 +292,7 @@ __device__ __forceinline__ void step_weights(float (&sc)[4][4], float qs, const 
     float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
     most = fmaxf(most, lane_xor<16>(most));
     most = fmaxf(most, lane_xor<32>(most)) * qs;
-    const bool grow = most > S.ref + kSlack;
+    const bool grow = most - S.ref > kSlack;                 // (the difference: their sum would be rounded, up as well)
     if (__any(grow)) {
         const float ref = grow ? most : S.ref, shrink = pow2(S.ref - (ref == -INFINITY ? 0.f : ref));    // (1 where nothing grows, or 0 * 0)
         S.ref = ref;

@@ -319,3 +319,24 @@ def test_gemm_of_large_row_scales(gpu, rows, n, k, gated):
     sure = (np.abs(want) < 3.3e38) & ((gate > 100) | (gate < -200))
     assert sure.any()
     assert (np.abs(got - want) <= 9 * U32 * np.abs(want) + 1e-37)[sure].all()
+
+
+@pytest.mark.parametrize("rows", [1, 70])
+def test_attention_of_large_scores_a_step_apart(gpu, rows):
+    """Scores of about 2^26.5 (in units of log2) that grow from one step of 64 keys to the next by the distance of neighbouring float32 numbers, 8 there:
+    more than a reference may be exceeded by, less than half a step of the sum of the two."""
+    torch, A = gpu
+    hd, n = 64, 512 + rows
+    for first in range(3):
+        k = np.zeros((n, 8, hd), np.float32)
+        k[..., :16] = 254                                     # 127 steps of 2
+        k[..., 16] = 2 * np.minimum(np.arange(n) // 64 + first, 126)[:, None]
+        v = np.random.default_rng(first).standard_normal((n, 8, hd)).astype(np.float32)
+        q = np.zeros((rows, 8, hd), np.float32)
+        q[..., :16], q[..., 16] = 131072, 16.125              # 32512 and 4 of the query's 16 bits
+        cache = A.Q8Cache(n_layers=1, n_seqs=1, n_q_heads=8, n_kv_heads=8, head_dim=hd, capacity=8192)     # chunks of 512
+        bf = lambda a: torch.from_numpy(a).to(torch.bfloat16).cuda()   # noqa: E731
+        _append(gpu, cache, [0], [0], [bf(k)], [bf(v)])
+        out, = _attend(gpu, cache, [0], [n - rows], [bf(q)], 0.125)
+        held = np.abs(_read(gpu, cache, 0, 0, n, 8, hd)[1]).max()
+        assert (np.abs(_np(out)) <= held * (1 + 2.0 ** -7)).all()          # a mean of values: no NaN, none past the largest

@@ -183,3 +183,37 @@ def test_quantize_many_long_rows_as_few(gpu, rows, n):
         got.append((q, s))
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
     assert (got[0][0].abs().amax(1) == 127).all().item()
+
+
+@pytest.mark.parametrize("hd,block", [(64, 1), (128, 64)])
+def test_attention_at_the_last_of_2_24_positions(gpu, hd, block):
+    """The longest cache: a window at its end, over zeros and a few keys there and at its beginning that outweigh them."""
+    torch, A = gpu
+    capacity, rows = 1 << 24, 3
+    cache = A.Q8Cache(n_layers=1, n_seqs=1, n_q_heads=2, n_kv_heads=1, head_dim=hd, capacity=capacity, block=block)
+    rng = np.random.default_rng(hd)
+    bf = lambda a: torch.from_numpy(a.astype(np.float32)).to(torch.bfloat16).cuda()   # noqa: E731
+    held = []
+    for at, n in ((0, 64), (capacity - 64, 64)):
+        k, v = bf(rng.standard_normal((n, hd)) * 1.5), bf(rng.standard_normal((n, hd)))
+        cache.append(0, [0], [at], [n], k.data_ptr(), v.data_ptr(), hd)
+        kk, vv = (torch.empty(n, hd, device="cuda") for _ in range(2))
+        cache.read(0, [0], [at], [n], kk.data_ptr(), vv.data_ptr(), A.DTYPE_FP32, hd)
+        held.append((kk.cpu().numpy().astype(np.float64), vv.cpu().numpy().astype(np.float64)))
+    q = bf(rng.standard_normal((rows, 2, hd)) * 12)
+    out, = _attend(gpu, cache, [0], [capacity - rows], [q], hd ** -0.5)
+    qn, got = q.float().cpu().numpy().astype(np.float64), out.float().cpu().numpy()
+    for r in range(rows):
+        k = np.concatenate([held[0][0], held[1][0][:64 - rows + r + 1]])
+        v = np.concatenate([held[0][1], held[1][1][:64 - rows + r + 1]])
+        s = qn[r] @ k.T * hd ** -0.5                                         # [2, keys]; all others are 0
+        top = np.maximum(s.max(1, keepdims=True), 0)
+        p = np.exp(s - top)
+        den = p.sum(1, keepdims=True) + (capacity - rows + r + 1 - len(k)) * np.exp(-top)
+        want, weighted = p @ v / den, p @ np.abs(v) / den
+        assert np.abs(want).max() > 0.1
+        # the scores' rounding (a query's 16 bits and seven of float32, twice), the weights' to half, 32768 chunks' sums one after the other
+        off = hd ** -0.5 * np.abs(k).sum(1).max() * np.abs(qn[r]).max() * (0.5 / 32512 + 7 * 2.0 ** -24)
+        assert off < 0.1
+        tol = 2.0 ** -8 * np.abs(want) + weighted * (2.0 ** -11 + 2 * 1.1 * off + 2 * 33300 * 2.0 ** -24) + 520 * 2.0 ** -24 * 1280 / 127 * np.abs(v).max()
+        assert (np.abs(got[r] - want) <= tol).all(), r
